@@ -12,7 +12,7 @@
  *     otherwise the library allocates nothing, frees nothing and never synchronises: all
  *     work is enqueued on `stream` (a hipStream_t passed as void*; NULL = the default
  *     stream) and is complete when that stream reaches the point after the call.
- *   - All device pointers must be 16-byte aligned.
+ *   - All device pointers must be 16-byte aligned (the int32 arrays of the paged cache: 4-byte).
  *   - Every call validates its arguments on the host before launching anything and
  *     returns an rtn_status; nothing aborts and nothing throws.  A HIP launch failure is
  *     reported as RTN_ERR_HIP.
@@ -301,6 +301,96 @@ int rtn_plan_bits(int layer, int n_layers, int module_id, int policy, int X, uns
  * module_params[i] = weights of module i+1 in one layer.  Returns -1 on invalid arguments. */
 double rtn_plan_effective_bits(int n_layers, const int64_t module_params[4], int policy, int X,
                                unsigned module_mask);
+
+/* ---- The attention block's cache.  Between the quantised QKV projection and the attention output projection of a layer (modules 1 and 2
+ * of Section 4.2) a step of token generation needs a place for each new token's K and V, the rotation of its queries and keys, and
+ * the attention over what its request has cached.  K and V live in pages of page_size tokens from a common pool, and a
+ * request's block table lists its pages; the three entry points below need no host copy of the lengths, so a step can be
+ * captured in a HIP graph and replayed while requests grow.
+ *
+ *   - Element types: fp16 and bf16 (RTN_TYPE_*), one for the cache and everything that is read or written with it.  (The quantised
+ *     linear layers take fp16.)  Indices and lengths are int32 and 4-byte aligned; everything else is 16-byte aligned.
+ *   - Values of tokens must be finite (NaN / Inf give unspecified results for their request).  Slots of a pool that hold no token of
+ *     the request may hold anything, NaN included: nothing of them reaches a result.
+ *   - Indices on the device are not known to the host and cannot be refused; those that would lead out of an array (a page that the
+ *     pool does not have, a length beyond the table) give unspecified results for their request, and no access out of bounds. */
+enum { RTN_TYPE_F16 = 0, RTN_TYPE_BF16 = 1 };
+
+/* K and V pools of one layer: element (page, head, token of the page, d) is at page * page_stride + head * head_stride +
+ * token * token_stride + d, in elements, in both.  page_size 16, 32, 64, 128 or 256; head_dim 64, 128 or 256; strides multiples of 8,
+ * token_stride >= head_dim and page_size * token_stride <= 2^30; pages * page_size < 2^31; up to 1024 kv_heads.
+ * [pages][kv_heads][page_size][head_dim] keeps a head's page in one piece; [pages][page_size][kv_heads][head_dim] a token's heads. */
+typedef struct {
+    void* dev_k;
+    void* dev_v;
+    int64_t pages;
+    int page_size, kv_heads, head_dim, dtype;
+    int64_t page_stride, head_stride, token_stride;
+} rtn_kv_cache;
+
+/* A step's block tables, slots and positions from the requests' lengths (once a step, for all layers).
+ * Request b has cached_lens[b] tokens.  step[b] >= 0 appends that many; step[b] < 0 ends the request: its pages go back and
+ * its length becomes 0.  Free pages are a stack, free_pages[0 .. free_count).  The pages of ended requests are pushed onto it in the order
+ * of requests and of their tables; then the appending requests pop the pages that they need, in the order of requests:
+ * need_b = ceil((cached + step) / page_size) - ceil(cached / page_size).
+ *   dev_step, dev_cached_lens   in   int32 [n_requests]
+ *   dev_block_table   in/out  int32, row b at b * table_stride, max_blocks entries; only new entries are written
+ *   dev_free_pages    in/out  int32 [pool]; entries from free_count on are written where more pages come back than go
+ *   dev_free_count    in   int32 [1]
+ *   dev_seq_lens      out  int32 [n_requests]: cached + step, 0 for ended requests
+ *   dev_query_start   out  int32 [n_requests + 1]: running sums of the tokens appended
+ *   dev_positions, dev_slots   out  int32 [max_tokens]: of new token query_start[b] + i: cached_lens[b] + i, and page * page_size + offset;
+ *                     -1 from query_start[n_requests] on
+ *   dev_free_count_out, dev_status   out  int32 [1]
+ * status: 0, or what does not fit, as a sum of 1 (pages), 2 (a row of the table), 4 (max_tokens), 8 (a length or count out of range:
+ * cached_lens, free_count, more pages back than the pool holds).  Then nothing happens: lengths and count stay, query_start is 0,
+ * positions and slots -1, table and stack are untouched.
+ * dev_seq_lens may be dev_cached_lens and dev_free_count_out may be dev_free_count, as a loop of replays wants it; no other buffers may
+ * overlap.  n_requests 1 .. 4096, max_tokens and pool below 2^30. */
+rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev_cached_lens, int n_requests, int page_size,
+                          int32_t* dev_block_table, int64_t table_stride, int max_blocks,
+                          int32_t* dev_free_pages, int64_t pool, const int32_t* dev_free_count,
+                          int32_t* dev_seq_lens, int32_t* dev_query_start, int32_t* dev_positions, int32_t* dev_slots, int64_t max_tokens,
+                          int32_t* dev_free_count_out, int32_t* dev_status, void* stream);
+
+/* Head norms, rotation and the cache write in one pass over the QKV projection's output.  A row of qkv holds q_heads query heads, then
+ * cache->kv_heads key heads, then as many value heads.  Query and key heads: x * rsqrt(mean(x^2) + eps) * weight where a weight is
+ * given; then the first rotary_dim elements are rotated in pairs (a, b) -> (a cos - b sin, b cos + a sin), pair i being elements
+ * (i, i + rotary_dim / 2), or (2 i, 2 i + 1) if interleaved, with cos at rope[position][i] and sin at rope[position][rotary_dim / 2 + i].
+ * All in fp32, rounded once.  Queries go to dev_q_out, keys and values to the cache's slot (page * page_size + offset); nothing
+ * is written to the cache for a slot < 0 (a padded batch) or beyond the pool.  Positions are clamped to the table.
+ *   dev_qkv        in   [tokens, (q_heads + 2 kv_heads) * head_dim], rows qkv_stride elements apart (a multiple of 8)
+ *   dev_rope       in   fp32 [max_positions, rotary_dim]; rotary_dim a multiple of 8, at most head_dim
+ *   dev_positions, dev_slots   in   int32 [tokens]; two tokens of a call must not have the same slot
+ *   dev_q_norm, dev_k_norm     in   [head_dim] in the cache's type, or NULL: no norm
+ *   dev_q_out      out  [tokens, q_heads, head_dim]
+ * tokens 0 .. 2^24 (0: nothing to do). */
+rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_t qkv_stride, int q_heads, const float* dev_rope, int rotary_dim,
+                          int64_t max_positions, int interleaved, const int32_t* dev_positions, const int32_t* dev_slots,
+                          const void* dev_q_norm, const void* dev_k_norm, float eps, const rtn_kv_cache* cache, void* dev_q_out, void* stream);
+
+/* Attention of the new tokens of a batch of requests over their pages (which hold the new tokens' K and V already): decode steps, drafted
+ * tokens, pieces of prompts and whole prompts, mixed at will.  Request b's new tokens are rows query_start[b] .. query_start[b + 1] - 1 and
+ * the last of its seq_lens[b] tokens; the one at position p sees key positions j <= p, and with window > 0 only those with p - j < window.
+ * Query head h reads KV head h / (q_heads / kv_heads).
+ *   out[t, h] = sum_j softmax_j(s_j) V_j,  s_j = scale q . K_j, or softcap tanh(scale q . K_j / softcap) if softcap > 0
+ * Scores, softmax and sums are fp32; the weights of V are rounded to the element type for the matrix cores.  A token that sees nothing
+ * (a length below the number of new tokens) gets zeros, and so do rows from query_start[n_requests] on (a padded batch).
+ * Pages that no new token of the request sees (outside every window) are not read: their table entries may be stale.
+ *   dev_q          in   [tokens, q_heads, head_dim], tokens q_stride elements apart (a multiple of 8)
+ *   dev_block_table    in   int32, row b at b * table_stride, max_blocks entries
+ *   dev_seq_lens, dev_query_start   in   int32 [n_requests], [n_requests + 1] (rising)
+ *   max_new        a bound on the new tokens of one request, from which the kernels are chosen: a wrong one costs time, not results
+ *   dev_out        out  [tokens, q_heads, head_dim]
+ *   dev_workspace  scratch, rtn_paged_attention_workspace_nbytes() bytes; with less or NULL long requests are not split over
+ *                  workgroups (slower, not an error); contents undefined before and after; calls that overlap in time need distinct ones
+ * q_heads a multiple of kv_heads, up to 64 times as many; tokens 0 .. 2^24; n_requests 1 .. 65536.  The same inputs with the same
+ * workspace size give the same bits. */
+size_t rtn_paged_attention_workspace_nbytes(int64_t tokens, int n_requests, int q_heads, const rtn_kv_cache* cache, int max_new);
+rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int64_t q_stride, int q_heads, const rtn_kv_cache* cache,
+                               const int32_t* dev_block_table, int64_t table_stride, int max_blocks, const int32_t* dev_seq_lens,
+                               const int32_t* dev_query_start, int n_requests, int max_new, float scale, float softcap, int window,
+                               void* dev_out, void* dev_workspace, size_t workspace_nbytes, void* stream);
 
 #ifdef __cplusplus
 }

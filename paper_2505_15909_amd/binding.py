@@ -6,6 +6,7 @@ the current stream, nothing else.  There is no fallback: if the library cannot b
 """
 from __future__ import annotations
 
+import collections
 import ctypes as C
 import os
 import sysconfig
@@ -35,6 +36,11 @@ class rtn_module(C.Structure):
     _fields_ = [("dev_A", C.c_void_p), ("M", C.c_int64), ("dev_qweight", C.c_void_p),
                 ("dev_scales", C.c_void_p), ("N", C.c_int64), ("K", C.c_int64),
                 ("bits", C.c_int), ("group_size", C.c_int), ("dev_C", C.c_void_p)]
+
+
+class rtn_kv_cache(C.Structure):
+    _fields_ = [("dev_k", C.c_void_p), ("dev_v", C.c_void_p), ("pages", C.c_int64), ("page_size", C.c_int), ("kv_heads", C.c_int),
+                ("head_dim", C.c_int), ("dtype", C.c_int), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
 
 
 def _load() -> C.CDLL:
@@ -96,6 +102,15 @@ def _load() -> C.CDLL:
     lib.rtn_plan_bits.argtypes = [ci, ci, ci, ci, ci, C.c_uint]
     lib.rtn_plan_effective_bits.restype = C.c_double
     lib.rtn_plan_effective_bits.argtypes = [ci, C.POINTER(i64), ci, ci, C.c_uint]
+    lib.rtn_cache_plan.restype = ci
+    lib.rtn_cache_plan.argtypes = [vp, vp, ci, ci, vp, i64, ci, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp]
+    lib.rtn_rope_cache.restype = ci
+    lib.rtn_rope_cache.argtypes = [vp, i64, i64, ci, vp, ci, i64, ci, vp, vp, vp, vp, C.c_float, C.POINTER(rtn_kv_cache), vp, vp]
+    lib.rtn_paged_attention_workspace_nbytes.restype = sz
+    lib.rtn_paged_attention_workspace_nbytes.argtypes = [i64, ci, ci, C.POINTER(rtn_kv_cache), ci]
+    lib.rtn_paged_attention.restype = ci
+    lib.rtn_paged_attention.argtypes = [vp, i64, i64, ci, C.POINTER(rtn_kv_cache), vp, i64, ci, vp, vp, ci, ci, C.c_float, C.c_float, ci,
+                                        vp, vp, sz, vp]
     return lib
 
 
@@ -125,7 +140,8 @@ EXPORTS = ["rtn_status_str", "rtn_layout_version", "rtn_qweight_nbytes", "rtn_sc
            "rtn_workspace_nbytes", "rtn_quantize", "rtn_quantize_host_staging_nbytes", "rtn_quantize_from_host", "rtn_linear", "rtn_linear_ex", "rtn_linear_query",
            "rtn_problem_status", "rtn_linear_validate", "rtn_linear_noalloc", "rtn_unpack", "rtn_dequantize", "rtn_gemm_fp16", "rtn_dense_weight_nbytes", "rtn_linear_dense",
            "rtn_quantize_asym", "rtn_dequantize_asym", "rtn_linear_asym",
-           "rtn_layer_forward", "rtn_grouped_forward", "rtn_bench_read_stream", "rtn_plan_bits", "rtn_plan_effective_bits"]
+           "rtn_layer_forward", "rtn_grouped_forward", "rtn_bench_read_stream", "rtn_plan_bits", "rtn_plan_effective_bits",
+           "rtn_cache_plan", "rtn_rope_cache", "rtn_paged_attention_workspace_nbytes", "rtn_paged_attention"]
 
 
 def _check(status: int, what: str):
@@ -423,3 +439,131 @@ def rtn_plan_effective_bits(n_layers, module_params, policy, X, modules=(1, 2, 3
     pol = POLICY[policy] if isinstance(policy, str) else policy
     arr = (C.c_int64 * 4)(*[int(v) for v in module_params])
     return _lib.rtn_plan_effective_bits(n_layers, arr, pol, X, mask)
+
+
+# ---- The paged KV cache: what a step of token generation does between the QKV projection and the attention output projection -----------
+
+RTN_TYPE_F16, RTN_TYPE_BF16 = 0, 1
+_TYPES = {torch.float16: RTN_TYPE_F16, torch.bfloat16: RTN_TYPE_BF16}
+
+
+class PagedCache:
+    """The K and V pools of one layer, [pages, kv_heads, page_size, head_dim] in fp16 or bf16: contiguous, or any view of that shape whose last
+    dimension is (pools stored [pages, page_size, kv_heads, head_dim] are passed as .transpose(1, 2))."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor):
+        if not (k.is_cuda and v.is_cuda and k.dim() == 4 and k.shape == v.shape and k.dtype == v.dtype and k.dtype in _TYPES and k.device == v.device):
+            raise ValueError("k and v must be CUDA tensors [pages, kv_heads, page_size, head_dim] of one type, fp16 or bf16")
+        if k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("k and v must have the same strides, with head_dim contiguous")
+        self.k, self.v = k, v
+        self.pages, self.kv_heads, self.page_size, self.head_dim = k.shape
+        self.dtype, self.device = k.dtype, k.device
+        self.desc = rtn_kv_cache(k.data_ptr(), v.data_ptr(), self.pages, self.page_size, self.kv_heads, self.head_dim, _TYPES[k.dtype],
+                                 k.stride(0), k.stride(1), k.stride(2))
+        self._ref = C.byref(self.desc)
+
+
+class CachePlan(collections.namedtuple("CachePlan", "seq_lens query_start positions slots free_count status")):
+    """What rtn_cache_plan gives, int32 on the GPU: seq_lens [requests], query_start [requests + 1], positions and slots [max_tokens],
+    free_count [1], status [1]."""
+    __slots__ = ()
+
+    @classmethod
+    def empty(cls, requests: int, max_tokens: int, device="cuda:0"):
+        return cls(*(torch.empty(n, dtype=torch.int32, device=device) for n in (requests, requests + 1, max_tokens, max_tokens, 1, 1)))
+
+
+def _dev_int32(t: torch.Tensor, name: str, n: int = None):
+    if not (t.is_cuda and t.dtype is torch.int32 and t.dim() == 1 and t.is_contiguous() and (n is None or t.shape[0] == n)):
+        raise ValueError(f"{name} must be a contiguous int32 CUDA vector" + ("" if n is None else f" of {n}"))
+
+
+def _dev_table(t: torch.Tensor):
+    if not (t.is_cuda and t.dtype is torch.int32 and t.dim() == 2 and t.stride(1) == 1):
+        raise ValueError("block_table must be an int32 CUDA matrix with contiguous rows")
+
+
+def _row_stride(t: torch.Tensor) -> int:
+    """Elements from row to row; a single row may have any stride."""
+    return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t[0].numel() if t.shape[0] else 0)
+
+
+def rtn_cache_plan(step: torch.Tensor, cached_lens: torch.Tensor, block_table: torch.Tensor, free_pages: torch.Tensor, free_count: torch.Tensor,
+                   page_size: int, max_tokens: int, out: CachePlan = None) -> CachePlan:
+    """A step's block tables, slots and positions: request b appends step[b] tokens to its cached_lens[b] (or ends, step[b] < 0), with pages
+    off the stack free_pages[:free_count].  block_table [requests, blocks] and free_pages are updated.  out.seq_lens may be cached_lens and
+    out.free_count free_count, for a loop of replays.  out.status says what did not fit (0: nothing), and then nothing has changed."""
+    _dev_int32(step, "step")
+    B = step.shape[0]
+    _dev_int32(cached_lens, "cached_lens", B)
+    _dev_int32(free_pages, "free_pages")
+    _dev_int32(free_count, "free_count", 1)
+    _dev_table(block_table)
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table must have a row for each of the {B} requests")
+    if out is None:
+        out = CachePlan.empty(B, max_tokens, step.device)
+    for t, name, n in zip(out, CachePlan._fields, (B, B + 1, max_tokens, max_tokens, 1, 1)):
+        _dev_int32(t, "out." + name, n)
+    _check(_lib.rtn_cache_plan(step.data_ptr(), cached_lens.data_ptr(), B, page_size, block_table.data_ptr(), _row_stride(block_table), block_table.shape[1],
+                               free_pages.data_ptr(), free_pages.shape[0], free_count.data_ptr(), out.seq_lens.data_ptr(), out.query_start.data_ptr(),
+                               out.positions.data_ptr(), out.slots.data_ptr(), max_tokens, out.free_count.data_ptr(), out.status.data_ptr(), _stream()),
+           "rtn_cache_plan")
+    return out
+
+
+def rtn_rope_cache(qkv: torch.Tensor, q_heads: int, rope: torch.Tensor, positions: torch.Tensor, slots: torch.Tensor, cache: PagedCache,
+                   q_norm: torch.Tensor = None, k_norm: torch.Tensor = None, eps: float = 1e-6, interleaved: bool = False,
+                   out: torch.Tensor = None) -> torch.Tensor:
+    """qkv [tokens, (q_heads + 2 kv_heads) * head_dim], the QKV projection's output -> queries [tokens, q_heads, head_dim], normed (where weights
+    are given) and rotated; keys, the same way, and values go to the cache's slots.  rope fp32 [positions, rotary_dim]: cosines, then sines."""
+    D, Hk, T = cache.head_dim, cache.kv_heads, qkv.shape[0]
+    if not (qkv.is_cuda and qkv.dtype is cache.dtype and qkv.dim() == 2 and qkv.shape[1] == (q_heads + 2 * Hk) * D and qkv.stride(1) == 1):
+        raise ValueError(f"qkv must be a CUDA matrix of the cache's type with {(q_heads + 2 * Hk) * D} contiguous columns")
+    if not (rope.is_cuda and rope.dtype is torch.float32 and rope.dim() == 2 and rope.is_contiguous()):
+        raise ValueError("rope must be a contiguous fp32 CUDA matrix [positions, rotary_dim]")
+    _dev_int32(positions, "positions", T)
+    _dev_int32(slots, "slots", T)
+    for w, name in ((q_norm, "q_norm"), (k_norm, "k_norm")):
+        if w is not None and not (w.is_cuda and w.dtype is cache.dtype and w.shape == (D,) and w.is_contiguous()):
+            raise ValueError(f"{name} must be a contiguous CUDA vector of {D} of the cache's type")
+    if out is None:
+        out = torch.empty((T, q_heads, D), dtype=cache.dtype, device=qkv.device)
+    elif not (out.is_cuda and out.dtype is cache.dtype and out.shape == (T, q_heads, D) and out.is_contiguous()):
+        raise ValueError("out must be a contiguous CUDA tensor [tokens, q_heads, head_dim] of the cache's type")
+    _check(_lib.rtn_rope_cache(qkv.data_ptr(), T, _row_stride(qkv), q_heads, rope.data_ptr(), rope.shape[1], rope.shape[0], int(interleaved),
+                               positions.data_ptr(), slots.data_ptr(), _ptr(q_norm), _ptr(k_norm), eps, cache._ref, out.data_ptr(), _stream()),
+           "rtn_rope_cache")
+    return out
+
+
+def rtn_paged_attention_workspace_nbytes(tokens: int, requests: int, q_heads: int, cache: PagedCache, max_new: int) -> int:
+    return _lib.rtn_paged_attention_workspace_nbytes(tokens, requests, q_heads, cache._ref, max_new)
+
+
+def rtn_paged_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.Tensor, seq_lens: torch.Tensor, query_start: torch.Tensor, max_new: int,
+                        scale: float = None, softcap: float = 0.0, window: int = 0, out: torch.Tensor = None,
+                        workspace: torch.Tensor = None) -> torch.Tensor:
+    """q [tokens, q_heads, head_dim], request b's new tokens being rows query_start[b] .. query_start[b + 1] - 1 and the last of its seq_lens[b]
+    tokens in the cache -> attention output of the same shape.  max_new: a bound on the new tokens of one request."""
+    T, Hq, D = q.shape
+    if not (q.is_cuda and q.dtype is cache.dtype and D == cache.head_dim and q.stride(2) == 1 and (q.stride(1) == D or Hq == 1)):
+        raise ValueError("q must be a CUDA tensor [tokens, q_heads, head_dim] of the cache's type, contiguous within a token")
+    _dev_int32(seq_lens, "seq_lens")
+    B = seq_lens.shape[0]
+    _dev_int32(query_start, "query_start", B + 1)
+    _dev_table(block_table)
+    if block_table.shape[0] != B:
+        raise ValueError(f"block_table must have a row for each of the {B} requests")
+    if out is None:
+        out = torch.empty((T, Hq, D), dtype=q.dtype, device=q.device)
+    elif not (out.is_cuda and out.dtype is q.dtype and out.shape == (T, Hq, D) and out.is_contiguous()):
+        raise ValueError("out must be a contiguous CUDA tensor of q's shape and type")
+    if workspace is None:
+        need = _lib.rtn_paged_attention_workspace_nbytes(T, B, Hq, cache._ref, max_new)
+        workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    _check(_lib.rtn_paged_attention(q.data_ptr(), T, _row_stride(q), Hq, cache._ref, block_table.data_ptr(), _row_stride(block_table), block_table.shape[1],
+                                    seq_lens.data_ptr(), query_start.data_ptr(), B, max_new, D ** -0.5 if scale is None else scale, softcap, window,
+                                    out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream()), "rtn_paged_attention")
+    return out
