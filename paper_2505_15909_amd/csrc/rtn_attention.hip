@@ -14,7 +14,7 @@
 namespace rtn {
 
 // Pieces that a batch is cut into where its tiles alone are fewer (see find_piece).
-constexpr int kPieces = 1024;
+constexpr int kPieces = 1024, kTilePieces = 512;
 
 struct AttnParams {
     const void *q, *k, *v;
@@ -249,6 +249,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
     const int32_t* const table = p.table + (int64_t)w.b * p.table_stride;
     const int ps = 1 << p.shift;
     // keys that every row sees need no masks
+    const int window = p.window ? p.window : 0x7FFFFFFF;     // (a position less this does not wrap: lengths are up to 2^30)
     const int all0 = p.window ? w.ctx + (w.row0 + w.rows - 1) / p.G - p.window + 1 : 0, all1 = w.ctx + w.row0 / p.G + 1;
     const int end = min(w.kv1, w.k1 * KEYS);
     int ids = 0;                                             // lane i: the page of the 16 keys that are number i of 64 this wavefront comes to
@@ -303,7 +304,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
                     const int key = k0 + 16 * (j >> 2) + 4 * grp + (j & 3);
-                    if (key > pos[n] || (p.window && pos[n] - key >= p.window)) e[j] = -INFINITY;
+                    e[j] = key > pos[n] || key <= pos[n] - window ? -INFINITY : e[j];
                 }
             }
 #pragma unroll
@@ -397,6 +398,211 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
     }
 }
 
+// Workgroup barrier behind a wavefront's loads into LDS and its reads.  (The builtin wait: the compiler counts on from it, where after one in
+// assembly it would have a stage's reads wait for the next stage's loads.)
+__device__ __forceinline__ void landed() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0x0070);                      // vmcnt(0) lgkmcnt(0)
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// Many rows: 128 of them a workgroup, 32 a wavefront, over blocks of KEYS keys that are staged in LDS, the next block on its way while one is
+// worked on.  Bound by the matrix cores and, about as much, by the exponentials: two workgroups share a compute unit, so that one's
+// products run beside the other's softmax.  Rows of a staged block are permuted by 16-byte pieces (K: by the key's last three
+// bits; V: four pieces at a time by its last two, or, two rows of 64 lying side by side, the second of them), which spreads what the matrix operands read over all banks; the loads into LDS, whose
+// destinations are in lane order, take their sources permuted instead.
+constexpr int kTileRows = 128;
+
+__device__ __align__(16) uint32_t attention_zeros[4];        // what a key outside the request has for V
+
+template <int TYPE, int D, int KEYS>
+__global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttnParams p) {
+    typedef typename Elem<TYPE>::one T;
+    typedef typename Elem<TYPE>::x8 T8;
+    typedef typename Elem<TYPE>::x4 T4;
+    constexpr int KS = D / 16, DT = D / 32, KT = KEYS / 32;  // k-steps of K Q^T, 32-row tiles of O^T, 32-key tiles of S^T
+    constexpr int CH = D / 8, PER = 64 / CH;                 // 16-byte pieces of a row, rows a load of a wavefront brings
+    constexpr int MINE = KEYS / 4, LOADS = MINE / PER;       // rows of a block that a wavefront brings, in so many loads
+    static_assert(LOADS >= 1 && MINE <= 16, "a wavefront's share of a block is in one page");
+    __shared__ __align__(16) uint8_t lds_k0[KEYS * D * 2], lds_k1[KEYS * D * 2], lds_v0[KEYS * D * 2], lds_v1[KEYS * D * 2];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
+    const int head = blockIdx.x % p.Hk;
+    clear_padding<256>(p, D);
+    Piece w;
+    if (!find_piece<kTileRows, KEYS, true>(p, blockIdx.x / p.Hk, &w)) return;
+
+    const int wrow = wave * 32, row = w.row0 + min(wrow + col, w.rows - 1), tok = row / p.G, qh = head * p.G + row - tok * p.G;
+    const int pos = w.ctx + tok;
+    T8 q[KS];
+    {
+        const T* const qp = static_cast<const T*>(p.q) + (int64_t)(w.tok0 + tok) * p.q_stride + (int64_t)qh * D + hi * 8;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) q[s] = *reinterpret_cast<const T8*>(qp + s * 16);
+    }
+    float16_t o[DT];
+#pragma unroll
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) o[t][j] = 0.f;
+    float m = -INFINITY, l = 0.f;
+    const int32_t* const table = p.table + (int64_t)w.b * p.table_stride;
+    const int ps = 1 << p.shift;
+    // keys that every row of this wavefront sees need no masks; those that none sees no work
+    const int lo_row = w.row0 + min(wrow, w.rows - 1), hi_row = w.row0 + min(wrow + 31, w.rows - 1);
+    const int pos_lo = w.ctx + __builtin_amdgcn_readfirstlane(lo_row / p.G), pos_hi = w.ctx + __builtin_amdgcn_readfirstlane(hi_row / p.G);
+    const int window = p.window ? p.window : 0x7FFFFFFF;
+    const int all0 = p.window ? pos_hi - p.window + 1 : 0, all1 = pos_lo + 1;
+    const int any0 = p.window ? pos_lo - p.window + 1 : 0, any1 = wrow < w.rows ? pos_hi + 1 : 0;
+
+    // sources of a wavefront's loads: rows MINE wave .. of a block, a lane's piece permuted back
+    uint32_t koff[LOADS], voff[LOADS];                       // in elements
+#pragma unroll
+    for (int j = 0; j < LOADS; ++j) {
+        const int r = j * PER + lane / CH, rr = MINE * wave + r, piece = lane % CH;
+        koff[j] = r * (uint32_t)p.token_stride + (piece ^ (rr & 7)) * 8;
+        voff[j] = r * (uint32_t)p.token_stride + (piece ^ (D == 64 ? (rr & 2) * 2 : (rr & 3) * 4)) * 8;
+    }
+    int ids = 0;
+    auto stage = [&](int block, uint8_t* kb, uint8_t* vb) {
+        const int key = block * KEYS + MINE * wave, i = block - w.k0;
+        if ((i & 63) == 0) {                                 // the pages of the next 64 blocks, none outside what is seen
+            const int at = min(max(key + lane * KEYS, w.kv0), w.kv1 - 1);
+            ids = min((uint32_t)table[at >> p.shift], (uint32_t)(p.pages - 1));
+        }
+        const int64_t page = __builtin_amdgcn_readlane(ids, i & 63);
+        const int64_t off = page * p.page_stride + head * p.head_stride + (int64_t)(key & (ps - 1)) * p.token_stride;
+        const T *const kp = static_cast<const T*>(p.k) + off, *const vp = static_cast<const T*>(p.v) + off;
+        const bool edge = key < w.kv0 || key + MINE > w.kv1;
+#pragma unroll
+        for (int j = 0; j < LOADS; ++j) {
+            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(kp + koff[j]),
+                                             (__attribute__((address_space(3))) void*)(kb + (MINE * wave + j * PER) * D * 2), 16, 0, 0);
+            const T* src = vp + voff[j];
+            if (edge) {                                      // slots without a token of the request may hold anything
+                const int k = key + j * PER + lane / CH;
+                if (k < w.kv0 || k >= w.kv1) src = reinterpret_cast<const T*>(attention_zeros);
+            }
+            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)src,
+                                             (__attribute__((address_space(3))) void*)(vb + (MINE * wave + j * PER) * D * 2), 16, 0, 0);
+        }
+    };
+    auto work = [&](int block, const uint8_t* kb, const uint8_t* vb) {
+        const int k0 = block * KEYS;
+        if (k0 >= any1 || k0 + KEYS <= any0) return;
+        float16_t s[KT];
+#pragma unroll
+        for (int h = 0; h < KT; ++h) {
+#pragma unroll
+            for (int j = 0; j < 16; ++j) s[h][j] = 0.f;
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                const T8 a = *reinterpret_cast<const T8*>(kb + (32 * h + col) * D * 2 + (((2 * t + hi) ^ (col & 7)) * 16));
+                s[h] = Elem<TYPE>::mfma32(a, q[t], s[h]);
+            }
+        }
+        float scale = p.scale2;
+        if (p.cap > 0.f) {
+            scale = 1.f;
+#pragma unroll
+            for (int h = 0; h < KT; ++h)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) s[h][j] = capped(s[h][j] * p.cap_in, p.cap_out);
+        }
+        if (k0 < all0 || k0 + KEYS > all1) {
+#pragma unroll
+            for (int h = 0; h < KT; ++h)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const int key = k0 + 32 * h + 8 * (j >> 2) + 4 * hi + (j & 3);
+                    s[h][j] = key > pos || key <= pos - window ? -INFINITY : s[h][j];
+                }
+        }
+        float top = -INFINITY;
+#pragma unroll
+        for (int h = 0; h < KT; ++h)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) top = fmaxf(top, s[h][j]);
+        top = fmaxf(top, __shfl_xor(top, 32)) * scale;
+        // The weights are relative to a maximum that is only followed where it has grown by 2^8: they stay below 2^8, exact to the same share, and the
+        // sums, most of the time, need no rescaling.
+        if (__any(top > m + 8.f)) {
+            const float m_new = fmaxf(m, top), back = m_new == -INFINITY ? 1.f : exp2_of(m - m_new);
+            m = m_new;
+            l *= back;
+#pragma unroll
+            for (int t = 0; t < DT; ++t)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) o[t][j] *= back;
+        }
+        const float base = m == -INFINITY ? 0.f : m;
+        T8 pt[KT * 2];
+#pragma unroll
+        for (int h = 0; h < KT; ++h)
+#pragma unroll
+            for (int j = 0; j < 16; ++j) {
+                const float x = exp2_of(fmaf(s[h][j], scale, -base));
+                l += x;
+                pt[2 * h + (j >> 3)][j & 7] = (T)x;          // (the weight of V in the element type: half an ulp of it, as much as the result's own rounding)
+            }
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int h = 0; h < KT * 2; ++h) {
+                union { T8 v; short4_t s[2]; } a;
+#pragma unroll
+                for (int x = 0; x < 2; ++x) {
+                    const int i = lane & 15, g = lane >> 4, key = 16 * h + 8 * x + 4 * (g >> 1) + (i >> 2);
+                    const int piece = (4 * t + 2 * (g & 1) + ((i & 3) >> 1)) ^ (D == 64 ? (key & 2) * 2 : (key & 3) * 4);
+                    a.s[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                        (__attribute__((address_space(3))) short4_t*)(vb + key * D * 2 + piece * 16 + (i & 1) * 8));
+                }
+                o[t] = Elem<TYPE>::mfma32(a.v, pt[h], o[t]);
+            }
+    };
+
+    // (the queries are waited for here: in the loop that would be a wait for the loads into LDS as well)
+#pragma unroll
+    for (int s = 0; s < KS; ++s) asm volatile("" : "+v"(q[s]));
+    if (w.k0 < w.k1) stage(w.k0, lds_k0, lds_v0);
+    for (int block = w.k0; block < w.k1; block += 2) {
+        landed();
+        if (block + 1 < w.k1) stage(block + 1, lds_k1, lds_v1);
+        work(block, lds_k0, lds_v0);
+        if (block + 1 >= w.k1) break;
+        landed();
+        if (block + 2 < w.k1) stage(block + 2, lds_k0, lds_v0);
+        work(block + 1, lds_k1, lds_v1);
+    }
+    l += __shfl_xor(l, 32);
+    if (wrow + col >= w.rows) return;
+    if (w.parts > 1) {
+        float* const po = partial_sums(p, head, w.slot + w.part, kTileRows, D) + (wrow + col) * D;
+        float* const st = partial_stats(p, head, w.slot + w.part, kTileRows, D) + (wrow + col) * 2;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4)
+                *reinterpret_cast<float4_t*>(po + t * 32 + 2 * j + 4 * hi) = (float4_t){o[t][j], o[t][j + 1], o[t][j + 2], o[t][j + 3]};
+        if (hi == 0) {
+            st[0] = m;
+            st[1] = l;
+        }
+    } else {
+        const float inv = l > 0.f ? 1.0f / l : 0.f;
+        T* const dst = static_cast<T*>(p.out) + ((int64_t)(w.tok0 + tok) * p.Hq + qh) * D;
+#pragma unroll
+        for (int t = 0; t < DT; ++t)
+#pragma unroll
+            for (int j = 0; j < 16; j += 4) {
+                T4 y;
+#pragma unroll
+                for (int x = 0; x < 4; ++x) y[x] = (T)(o[t][j + x] * inv);
+                *reinterpret_cast<T4*>(dst + t * 32 + 2 * j + 4 * hi) = y;
+            }
+    }
+}
+
 // The launch for a call: tiles of 16 or 32 rows, and the pieces aimed at.  Bytes of a partial result of one KV head: rows (D + 2) floats.
 struct AttnPlan {
     int rows, pieces;
@@ -407,8 +613,9 @@ struct AttnPlan {
 static AttnPlan plan_attention(int64_t T, int B, int Hq, int Hk, int D, int max_new) {
     const int G = Hq / Hk;
     AttnPlan a;
-    a.rows = (int64_t)max_new * G <= 16 || D == 256 ? 16 : 32;
-    a.pieces = (kPieces + Hk - 1) / Hk;
+    const int64_t rows = (int64_t)max_new * G;
+    a.rows = rows > 64 ? kTileRows : rows <= 16 || D == 256 ? 16 : 32;
+    a.pieces = ((a.rows == kTileRows ? kTilePieces : kPieces) + Hk - 1) / Hk;
     return a;
 }
 
@@ -421,6 +628,13 @@ static void launch_rows(const AttnParams& p, hipStream_t st) {
 
 template <int TYPE, int D>
 static void launch_attention(const AttnParams& p, const AttnPlan& a, hipStream_t st) {
+    if (a.rows == kTileRows) {
+        constexpr int KEYS = D == 256 ? 32 : 64;
+        const int64_t tiles = (int64_t)p.T * p.G / kTileRows + p.B;
+        hipLaunchKernelGGL((attend_tiles_kernel<TYPE, D, KEYS>), dim3((unsigned)((tiles + p.pieces) * p.Hk)), dim3(256), 0, st, p);
+        if (p.pieces) hipLaunchKernelGGL((join_parts_kernel<TYPE, D, kTileRows, KEYS>), dim3((unsigned)(tiles * p.Hk)), dim3(256), 0, st, p);
+        return;
+    }
     if constexpr (D < 256) {
         if (a.rows == 32) return launch_rows<TYPE, D, 2>(p, st);
     }
