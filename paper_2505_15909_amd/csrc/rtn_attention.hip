@@ -9,12 +9,20 @@
 // O^T = V^T P^T, if V's keys are taken in the same order.  V^T's operands come out of LDS by transposing reads.
 #include "rtn_paged.h"
 
+#include <algorithm>
 #include <math.h>
 
 namespace rtn {
 
-// Pieces that a batch is cut into where its tiles alone are fewer (see find_piece).
-constexpr int kPieces = 1024, kTilePieces = 512;
+// Requests of up to kFew rows go to the workgroups for few rows, longer ones to those for many (kTileRows).
+constexpr int kFew = 64, kTileRows = 128;
+
+// One of the two kinds of workgroups in a launch.  `pieces` a KV head are aimed at (0: no request is split), and a head has room for twice as many
+// partial results, [Hk][2 pieces][rows][D] sums and, behind them, [Hk][2 pieces][rows][2] maxima and sums of weights.
+struct AttnKind {
+    float* partial;
+    int pieces, most;                                        // most: a bound on the pieces of a KV head
+};
 
 struct AttnParams {
     const void *q, *k, *v;
@@ -23,10 +31,8 @@ struct AttnParams {
     int64_t q_stride, page_stride, head_stride, token_stride, table_stride;
     int pages, shift, max_blocks, B, T, Hq, Hk, G, window;
     float scale2, cap, cap_in, cap_out;                      // scale log2 e; softcap: cap_out tanh(cap_in q.k), cap_out = softcap log2 e
-    // Split requests: `pieces` a KV head are aimed at (0: none is split), and a head has room for twice as many partial results,
-    // [Hk][2 pieces][rows][D] sums and, behind them, [Hk][2 pieces][rows][2] maxima and sums of weights.
-    float* partial;
-    int pieces;
+    int few_rows;                                            // kFew, or no bound where the call's requests are all taken to have few
+    AttnKind few, many;
 };
 
 // exp2 of scores: the softmax is taken to base 2, with log2 e in the scale
@@ -43,33 +49,38 @@ struct Piece {
     int b, row0, rows, tok0, n, ctx;                         // rows of the tile, first token in the batch, new tokens, cached tokens
     int kv0, kv1;                                            // keys that some row sees
     int part, parts, slot;                                   // of the tile's keys; where the first part's partial result goes
-    int k0, k1;                                              // this part's, in blocks of KEYS from kv0's
+    int k0, k1;                                              // this part's, in blocks of KEYS
 };
 
 // Each workgroup finds its own piece from the requests' lengths, which the host does not know: with n_b blocks of keys and t_b
 // tiles of rows, pieces of c = ceil(sum t_b n_b / `pieces`) blocks put a like share of the whole batch's keys on every workgroup, whatever the
-// requests' lengths; tile t of request b has the t_b ceil(n_b / c) pieces after those of the requests before it.  Two scans over the requests, a
-// microsecond or two.  PART: number `no` of the pieces; otherwise of the tiles (what joins the parts).  All 256 threads call it.
-template <int ROWS, int KEYS, bool PART>
-__device__ __forceinline__ bool find_piece(const AttnParams& p, int no, Piece* out) {
+// requests' lengths; tile t of request b has the t_b ceil(n_b / c) pieces after those of the requests before it.  Two scans over the requests, each
+// thread's (one, up to 256 of them) read once.  `no` counts the pieces, or, JOIN, those of split requests alone.  All 256 threads call it.
+template <int ROWS, int KEYS, bool JOIN>
+__device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int no, Piece* out) {
     __shared__ int64_t totals[4];
-    __shared__ int sums[4][2], found[4];
+    __shared__ int sums[4][2], found[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (p.B + 255) / 256, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     struct Request { int tok0, n, seq, tiles, blocks; };
-    auto request = [&](int b) {
+    auto read = [&](int b) {
         Request r;
-        r.tok0 = min(max(p.start[b], 0), p.T);
-        r.n = min(max(p.start[b + 1], r.tok0), p.T) - r.tok0;
-        r.seq = min(max(p.seq[b], 0), p.max_blocks << p.shift);
-        r.tiles = (r.n * p.G + ROWS - 1) / ROWS;
+        const int s = p.start[b], e = p.start[b + 1], len = p.seq[b];
+        r.tok0 = min(max(s, 0), p.T);
+        r.n = min(max(e, r.tok0), p.T) - r.tok0;
+        r.seq = min(max(len, 0), p.max_blocks << p.shift);
+        const int rows = r.n * p.G;
+        r.tiles = (rows > p.few_rows) == (ROWS > kFew) ? (rows + ROWS - 1) / ROWS : 0;
         // (with a window, a bound on what a tile sees: the windows of its tokens, unaligned)
         r.blocks = (r.seq + KEYS - 1) / KEYS;
         if (p.window) r.blocks = (int)min((int64_t)r.blocks, ((int64_t)p.window + ROWS / p.G + 1 + KEYS - 1) / KEYS + 1);
         return r;
     };
+    Request own = {};
+    if (b0 < b1) own = read(b0);
+    auto request = [&](int b) { return b == b0 ? own : read(b); };
     int c = 0x7FFFFFFF;
-    if (p.pieces) {
+    if (pieces) {
         int64_t total = 0;
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
@@ -80,14 +91,14 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int no, Piece* o
         if (lane == 0) totals[wave] = total;
         __syncthreads();
         total = totals[0] + totals[1] + totals[2] + totals[3];
-        c = (int)min((int64_t)0x7FFFFFFF, max((int64_t)1, (total + p.pieces - 1) / p.pieces));
+        c = (int)min((int64_t)0x7FFFFFFF, max((int64_t)1, (total + pieces - 1) / pieces));
     }
     auto parts_of = [&](int blocks) { return max(1, (int)(((int64_t)blocks + c - 1) / c)); };
-    int mine[2] = {0, 0};                                    // numbers (of pieces or tiles), slots
+    int mine[2] = {0, 0};                                    // pieces, and those of split requests
     for (int b = b0; b < b1; ++b) {
         const Request r = request(b);
         const int parts = parts_of(r.blocks);
-        mine[0] += PART ? r.tiles * parts : r.tiles;
+        mine[0] += r.tiles * parts;
         mine[1] += parts > 1 ? r.tiles * parts : 0;
     }
     int incl[2] = {mine[0], mine[1]};
@@ -110,52 +121,55 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int no, Piece* o
         before += sums[w][0];
         slot += sums[w][1];
     }
-    if (no >= before && no < before + mine[0]) {
+    if (JOIN) before = slot;
+    if (no >= before && no < before + mine[JOIN ? 1 : 0]) {
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
-            const int parts = parts_of(r.blocks), have = PART ? r.tiles * parts : r.tiles;
+            const int parts = parts_of(r.blocks), slots = parts > 1 ? r.tiles * parts : 0, have = JOIN ? slots : r.tiles * parts;
             if (no < before + have) {
                 found[0] = b;
                 found[1] = no - before;
                 found[2] = slot;
                 found[3] = parts;
+                found[4] = r.tok0;
+                found[5] = r.n;
+                found[6] = r.seq;
                 break;
             }
             before += have;
-            slot += parts > 1 ? r.tiles * parts : 0;
+            slot += slots;
         }
     }
     __syncthreads();
-    const int b = __builtin_amdgcn_readfirstlane(found[0]);
-    if (b < 0) return false;
+    out->b = __builtin_amdgcn_readfirstlane(found[0]);
+    if (out->b < 0) return false;
     const int local = __builtin_amdgcn_readfirstlane(found[1]), most = __builtin_amdgcn_readfirstlane(found[3]);
-    const Request r = request(b);
-    const int tile = PART ? local / most : local;
-    out->b = b;
-    out->tok0 = r.tok0;
-    out->n = r.n;
-    out->ctx = r.seq - r.n;
+    const int tiles = (__builtin_amdgcn_readfirstlane(found[5]) * p.G + ROWS - 1) / ROWS, nth = local / most;
+    const int tile = tiles - 1 - nth;                        // the last rows see most keys: they come first
+    out->tok0 = __builtin_amdgcn_readfirstlane(found[4]);
+    out->n = __builtin_amdgcn_readfirstlane(found[5]);
+    out->ctx = __builtin_amdgcn_readfirstlane(found[6]) - out->n;
     out->row0 = tile * ROWS;
-    out->rows = min(ROWS, r.n * p.G - out->row0);
+    out->rows = min(ROWS, out->n * p.G - out->row0);
     const int first = out->ctx + out->row0 / p.G, last = out->ctx + (out->row0 + out->rows - 1) / p.G;
     out->kv0 = p.window ? max(0, first - p.window + 1) : 0;
     out->kv1 = last + 1;                                     // (not above the length; 0 and less where nothing is seen)
     // the tile's own blocks, which may be fewer than its request's: as many parts as they fill, of like size
     const int blocks = max(0, (out->kv1 + KEYS - 1) / KEYS - out->kv0 / KEYS);
     out->parts = min(most, parts_of(blocks));
-    out->part = PART ? local - tile * most : 0;
-    out->slot = __builtin_amdgcn_readfirstlane(found[2]) + tile * most;
+    out->part = local - nth * most;
+    out->slot = __builtin_amdgcn_readfirstlane(found[2]) + nth * most;
     const int each = (blocks + out->parts - 1) / out->parts;
     out->k0 = out->kv0 / KEYS + out->part * each;
     out->k1 = min(out->k0 + each, out->kv0 / KEYS + blocks);
     return out->part < out->parts;
 }
 
-__device__ __forceinline__ float* partial_sums(const AttnParams& p, int head, int slot, int rows, int D) {
-    return p.partial + ((int64_t)head * 2 * p.pieces + slot) * rows * D;
+__device__ __forceinline__ float* partial_sums(const AttnParams& p, const AttnKind& kind, int head, int slot, int rows, int D) {
+    return kind.partial + ((int64_t)head * 2 * kind.pieces + slot) * rows * D;
 }
-__device__ __forceinline__ float* partial_stats(const AttnParams& p, int head, int slot, int rows, int D) {
-    return p.partial + (int64_t)p.Hk * 2 * p.pieces * rows * D + ((int64_t)head * 2 * p.pieces + slot) * rows * 2;
+__device__ __forceinline__ float* partial_stats(const AttnParams& p, const AttnKind& kind, int head, int slot, int rows, int D) {
+    return kind.partial + (int64_t)p.Hk * 2 * kind.pieces * rows * D + ((int64_t)head * 2 * kind.pieces + slot) * rows * 2;
 }
 
 // Rows of a padded batch get zeros: every workgroup a share, whatever it does else.
@@ -166,36 +180,59 @@ __device__ __forceinline__ void clear_padding(const AttnParams& p, int D) {
         reinterpret_cast<u32x4_t*>(p.out)[i] = (u32x4_t){0u, 0u, 0u, 0u};
 }
 
-// The parts of a tile's keys, brought to their common maximum and added up in their order.
+// The parts of a tile's keys, brought to their common maximum and added up.  The workgroups of a tile, as many as it has parts, share its rows.
+// D / 4 threads take a row's sums of a part: 1024 / D parts or, of fewer parts, several rows at a time.
 template <int TYPE, int D, int ROWS, int KEYS>
-__global__ __launch_bounds__(256) void join_parts_kernel(const AttnParams p) {
+__device__ __forceinline__ void join_parts(const AttnParams& p, const AttnKind& kind, int block) {
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x4 T4;
-    const int head = blockIdx.x % p.Hk;
+    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    __shared__ __align__(16) float sums[GROUPS][D];
+    __shared__ float stats[GROUPS][2];
+    const int head = block % p.Hk, lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     Piece w;
-    if (!find_piece<ROWS, KEYS, false>(p, blockIdx.x / p.Hk, &w) || w.parts == 1) return;
-    const float *const po = partial_sums(p, head, w.slot, ROWS, D), *const pm = partial_stats(p, head, w.slot, ROWS, D);
-    for (int i = threadIdx.x; i < w.rows * (D / 4); i += 256) {
-        const int r = i / (D / 4), d = i % (D / 4) * 4;
-        float top = -INFINITY;
-        for (int s = 0; s < w.parts; ++s) top = fmaxf(top, pm[((int64_t)s * ROWS + r) * 2]);
-        const float base = top == -INFINITY ? 0.f : top;
+    if (!find_piece<ROWS, KEYS, true>(p, kind.pieces, block / p.Hk, &w) || w.parts == 1) return;
+    const float *const po = partial_sums(p, kind, head, w.slot, ROWS, D) + lane * 4, *const pm = partial_stats(p, kind, head, w.slot, ROWS, D);
+    const int r0 = w.rows * w.part / w.parts, r1 = w.rows * (w.part + 1) / w.parts;
+    int by_parts = 1;                                        // groups that share a row
+    while (by_parts < GROUPS && by_parts < w.parts) by_parts *= 2;
+    const int at_once = GROUPS / by_parts, first = group & (by_parts - 1);
+    for (int r = r0 + group / by_parts; r < r1 + at_once - 1; r += at_once) {      // (as many turns for all groups)
         float4_t acc = {0.f, 0.f, 0.f, 0.f};
-        float den = 0.f;
+        float m = -INFINITY, l = 0.f;
+        auto add = [&](float m2, float l2, const float4_t& x) {
+            const float top = fmaxf(m, m2), base = top == -INFINITY ? 0.f : top, f = exp2_of(m - base), g = exp2_of(m2 - base);
+            l = l * f + l2 * g;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) acc[j] = acc[j] * f + x[j] * g;
+            m = top;
+        };
+        if (r < r1) {
 #pragma unroll 4
-        for (int s = 0; s < w.parts; ++s) {
-            const float f = exp2_of(pm[((int64_t)s * ROWS + r) * 2] - base);
-            den += f * pm[((int64_t)s * ROWS + r) * 2 + 1];
-            const float4_t x = *reinterpret_cast<const float4_t*>(po + ((int64_t)s * ROWS + r) * D + d);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) acc[j] += f * x[j];
+            for (int s = first; s < w.parts; s += by_parts) {
+                const float2 st = *reinterpret_cast<const float2*>(pm + ((int64_t)s * ROWS + r) * 2);
+                add(st.x, st.y, *reinterpret_cast<const float4_t*>(po + ((int64_t)s * ROWS + r) * D));
+            }
         }
-        const float inv = den > 0.f ? 1.0f / den : 0.f;
-        const int row = w.row0 + r, tok = row / p.G;
-        T4 y;
+        if (by_parts > 1) {
+            *reinterpret_cast<float4_t*>(&sums[group][lane * 4]) = acc;
+            if (lane == 0) {
+                stats[group][0] = m;
+                stats[group][1] = l;
+            }
+            __syncthreads();
+            if (first == 0)
+                for (int g = 1; g < by_parts; ++g) add(stats[group + g][0], stats[group + g][1], *reinterpret_cast<const float4_t*>(&sums[group + g][lane * 4]));
+            __syncthreads();
+        }
+        if (first == 0 && r < r1) {
+            const float inv = l > 0.f ? 1.0f / l : 0.f;
+            const int row = w.row0 + r, tok = row / p.G;
+            T4 y;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) y[j] = (T)(acc[j] * inv);
-        *reinterpret_cast<T4*>(static_cast<T*>(p.out) + ((int64_t)(w.tok0 + tok) * p.Hq + head * p.G + row - tok * p.G) * D + d) = y;
+            for (int j = 0; j < 4; ++j) y[j] = (T)(acc[j] * inv);
+            *reinterpret_cast<T4*>(static_cast<T*>(p.out) + ((int64_t)(w.tok0 + tok) * p.Hq + head * p.G + row - tok * p.G) * D + lane * 4) = y;
+        }
     }
 }
 
@@ -207,24 +244,23 @@ __device__ __forceinline__ void wave_sync() {
 }
 
 // Few rows: 16 NQ of them a workgroup, whose four wavefronts take blocks of 32 keys in turn, each with a softmax of its own until they join
-// at the end.  Bound by the reading of K and V: K goes from memory into the matrix cores' registers, V by way of 8 KiB of LDS
-// that only its wavefront touches, so that the loop has no barrier.
+// at the end.  Bound by the reading of K and V, which go through LDS one after the other, 8 KiB that only its wavefront touches (D = 128), so that
+// the loop has no barrier.
+constexpr int few_lds_bytes(int D) { return 16 * (D + 4) * 4; }        // of a wavefront: 32 rows of V, and, later, sums of 16 rows
+
 template <int TYPE, int D, int NQ>
-__global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) void attend_rows_kernel(const AttnParams p) {
+__device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8_t* const (&buf)[4]) {
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x8 T8;
     typedef typename Elem<TYPE>::x4 T4;
     constexpr int KS = D / 32, DT = D / 16, STEP = 32, ROWS = 16 * NQ, KEYS = 4 * STEP;     // k-steps of K Q^T, 16-row tiles of O^T, keys of a step
     constexpr int SW_SHIFT = D == 64 ? 1 : 0, SW_MASK = D == 64 ? 3 : 7;
     constexpr int VI = STEP * D * 2 / 1024, CH = D / 8;      // loads of V, 16-byte pieces of a row
-    constexpr int MERGE = 16 * (D + 4) * 4;                  // bytes of a wavefront's sums of 16 rows, in place of its V
-    __shared__ __align__(16) uint8_t buf[4][MERGE > STEP * D * 2 ? MERGE : STEP * D * 2];
     __shared__ float stats[4][2][ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
-    const int head = blockIdx.x % p.Hk;
-    clear_padding<256>(p, D);
+    const int head = block % p.Hk;
     Piece w;
-    if (!find_piece<ROWS, KEYS, true>(p, blockIdx.x / p.Hk, &w)) return;
+    if (!find_piece<ROWS, KEYS, false>(p, p.few.pieces, block / p.Hk, &w)) return;
 
     T8 q[NQ][KS];
     int pos[NQ];                                             // (negative where the length is below the number of new tokens)
@@ -245,7 +281,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[n][t] = (float4_t){0.f, 0.f, 0.f, 0.f};
     }
-    uint8_t* const vb = buf[wave];
+    uint8_t* const vb = wave == 0 ? buf[0] : wave == 1 ? buf[1] : wave == 2 ? buf[2] : buf[3];
     const int32_t* const table = p.table + (int64_t)w.b * p.table_stride;
     const int ps = 1 << p.shift;
     // keys that every row sees need no masks
@@ -267,39 +303,43 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
             kt[h] = static_cast<const T*>(p.k) + off;
             vt[h] = static_cast<const T*>(p.v) + off;
         }
-        T8 k[2][KS];
+        // Whole rows by neighbouring lanes, as streaming: half rows, as the matrix cores take K, read 5 to 10 % slower.
+        auto load = [&](u32x4_t (&x)[VI], const T* const (&from)[2]) {
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int t = 0; t < KS; ++t) k[h][t] = *reinterpret_cast<const T8*>(kt[h] + col * (int)p.token_stride + t * 32 + grp * 8);
-        u32x4_t v[VI];
+            for (int j = 0; j < VI; ++j) {
+                const int key = (j * 64 + lane) / CH, piece = lane % CH;
+                x[j] = load_stream16(from[j * 64 / CH >> 4] + (key & 15) * (int)p.token_stride + piece * 8);
+            }
+        };
+        u32x4_t k[VI], v[VI];
+        load(k, kt);
+        if constexpr (D < 256) load(v, vt);
 #pragma unroll
         for (int j = 0; j < VI; ++j) {
             const int key = (j * 64 + lane) / CH, piece = lane % CH;
-            v[j] = *reinterpret_cast<const u32x4_t*>(vt[j * 64 / CH >> 4] + (key & 15) * (int)p.token_stride + piece * 8);
+            *reinterpret_cast<u32x4_t*>(vb + key * (D * 2) + (piece ^ (key & 7)) * 16) = k[j];
         }
-        if (k0 < w.kv0 || k0 + STEP > w.kv1) {               // slots without a token of the request may hold anything
+        wave_sync();
+        float4_t s[NQ][2];
 #pragma unroll
-            for (int j = 0; j < VI; ++j) {
-                const int key = k0 + (j * 64 + lane) / CH;
-                if (key < w.kv0 || key >= w.kv1) v[j] = (u32x4_t){0u, 0u, 0u, 0u};
+        for (int n = 0; n < NQ; ++n) s[n][0] = s[n][1] = (float4_t){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int t = 0; t < KS; ++t) {
+                const T8 a = *reinterpret_cast<const T8*>(vb + (16 * h + col) * (D * 2) + ((4 * t + grp) ^ (col & 7)) * 16);
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) s[n][h] = Elem<TYPE>::mfma16(a, q[n][t], s[n][h]);
             }
-        }
+        wave_sync();
         const bool masked = k0 < all0 || k0 + STEP > all1;
         T8 pt[NQ];
         float back[NQ];
 #pragma unroll
         for (int n = 0; n < NQ; ++n) {
-            float4_t s[2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                s[h] = (float4_t){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int t = 0; t < KS; ++t) s[h] = Elem<TYPE>::mfma16(k[h][t], q[n][t], s[h]);
-            }
             float e[8], top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = p.cap > 0.f ? capped(s[j >> 2][j & 3] * p.cap_in, p.cap_out) : s[j >> 2][j & 3] * p.scale2;
+            for (int j = 0; j < 8; ++j) e[j] = p.cap > 0.f ? capped(s[n][j >> 2][j & 3] * p.cap_in, p.cap_out) : s[n][j >> 2][j & 3] * p.scale2;
             if (masked) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -320,6 +360,14 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
                 const float x = exp2_of(e[j] - base);
                 l[n] += x;
                 pt[n][j] = (T)x;                             // (the weight of V in the element type: half an ulp of it, as much as the result's own rounding)
+            }
+        }
+        if constexpr (D == 256) load(v, vt);                 // (not beside K: 128 registers)
+        if (k0 < w.kv0 || k0 + STEP > w.kv1) {               // slots without a token of the request may hold anything
+#pragma unroll
+            for (int j = 0; j < VI; ++j) {
+                const int key = k0 + (j * 64 + lane) / CH;
+                if (key < w.kv0 || key >= w.kv1) v[j] = (u32x4_t){0u, 0u, 0u, 0u};
             }
         }
 #pragma unroll
@@ -380,9 +428,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) voi
                 for (int j = 0; j < 4; ++j) acc[j] += f * y[j];
             }
             if (w.parts > 1) {
-                *reinterpret_cast<float4_t*>(partial_sums(p, head, w.slot + w.part, ROWS, D) + (16 * n + r) * D + d) = acc;
+                *reinterpret_cast<float4_t*>(partial_sums(p, p.few, head, w.slot + w.part, ROWS, D) + (16 * n + r) * D + d) = acc;
                 if (d == 0) {
-                    float* const st = partial_stats(p, head, w.slot + w.part, ROWS, D) + (16 * n + r) * 2;
+                    float* const st = partial_stats(p, p.few, head, w.slot + w.part, ROWS, D) + (16 * n + r) * 2;
                     st[0] = top;
                     st[1] = den;
                 }
@@ -412,25 +460,23 @@ __device__ __forceinline__ void landed() {
 // products run beside the other's softmax.  Rows of a staged block are permuted by 16-byte pieces (K: by the key's last three
 // bits; V: four pieces at a time by its last two, or, two rows of 64 lying side by side, the second of them), which spreads what the matrix operands read over all banks; the loads into LDS, whose
 // destinations are in lane order, take their sources permuted instead.
-constexpr int kTileRows = 128;
-
 __device__ __align__(16) uint32_t attention_zeros[4];        // what a key outside the request has for V
 
-template <int TYPE, int D, int KEYS>
-__global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttnParams p) {
+constexpr int tile_keys(int D) { return D == 256 ? 32 : 64; }
+
+template <int TYPE, int D>
+__device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, uint8_t* lds_k0, uint8_t* lds_k1, uint8_t* lds_v0, uint8_t* lds_v1) {
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x8 T8;
     typedef typename Elem<TYPE>::x4 T4;
-    constexpr int KS = D / 16, DT = D / 32, KT = KEYS / 32;  // k-steps of K Q^T, 32-row tiles of O^T, 32-key tiles of S^T
+    constexpr int KEYS = tile_keys(D), KS = D / 16, DT = D / 32, KT = KEYS / 32;  // k-steps of K Q^T, 32-row tiles of O^T, 32-key tiles of S^T
     constexpr int CH = D / 8, PER = 64 / CH;                 // 16-byte pieces of a row, rows a load of a wavefront brings
     constexpr int MINE = KEYS / 4, LOADS = MINE / PER;       // rows of a block that a wavefront brings, in so many loads
     static_assert(LOADS >= 1 && MINE <= 16, "a wavefront's share of a block is in one page");
-    __shared__ __align__(16) uint8_t lds_k0[KEYS * D * 2], lds_k1[KEYS * D * 2], lds_v0[KEYS * D * 2], lds_v1[KEYS * D * 2];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
-    const int head = blockIdx.x % p.Hk;
-    clear_padding<256>(p, D);
+    const int head = block_no % p.Hk;
     Piece w;
-    if (!find_piece<kTileRows, KEYS, true>(p, blockIdx.x / p.Hk, &w)) return;
+    if (!find_piece<kTileRows, KEYS, false>(p, p.many.pieces, block_no / p.Hk, &w)) return;
 
     const int wrow = wave * 32, row = w.row0 + min(wrow + col, w.rows - 1), tok = row / p.G, qh = head * p.G + row - tok * p.G;
     const int pos = w.ctx + tok;
@@ -577,8 +623,8 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttnParams p
     l += __shfl_xor(l, 32);
     if (wrow + col >= w.rows) return;
     if (w.parts > 1) {
-        float* const po = partial_sums(p, head, w.slot + w.part, kTileRows, D) + (wrow + col) * D;
-        float* const st = partial_stats(p, head, w.slot + w.part, kTileRows, D) + (wrow + col) * 2;
+        float* const po = partial_sums(p, p.many, head, w.slot + w.part, kTileRows, D) + (wrow + col) * D;
+        float* const st = partial_stats(p, p.many, head, w.slot + w.part, kTileRows, D) + (wrow + col) * 2;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
 #pragma unroll
@@ -603,42 +649,83 @@ __global__ __launch_bounds__(256, 2) void attend_tiles_kernel(const AttnParams p
     }
 }
 
-// The launch for a call: tiles of 16 or 32 rows, and the pieces aimed at.  Bytes of a partial result of one KV head: rows (D + 2) floats.
+template <int TYPE, int D, int NQ>
+__global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) void attend_few_kernel(const AttnParams p) {
+    __shared__ __align__(16) uint8_t lds[4][few_lds_bytes(D)];
+    uint8_t* const buf[4] = {lds[0], lds[1], lds[2], lds[3]};
+    clear_padding<256>(p, D);
+    attend_few<TYPE, D, NQ>(p, blockIdx.x, buf);
+}
+
+// Requests of few rows and of many in one launch: the tiles' products run beside the others' reading.
+template <int TYPE, int D>
+__global__ __launch_bounds__(256, 2) void attend_mixed_kernel(const AttnParams p) {
+    constexpr int STAGE = tile_keys(D) * D * 2, BYTES = STAGE > few_lds_bytes(D) ? STAGE : few_lds_bytes(D);
+    __shared__ __align__(16) uint8_t lds_k0[BYTES], lds_k1[BYTES], lds_v0[BYTES], lds_v1[BYTES];
+    clear_padding<256>(p, D);
+    const int tiles = p.many.most * p.Hk;
+    if ((int)blockIdx.x < tiles) {
+        attend_many<TYPE, D>(p, blockIdx.x, lds_k0, lds_k1, lds_v0, lds_v1);
+    } else {
+        uint8_t* const buf[4] = {lds_k0, lds_k1, lds_v0, lds_v1};
+        attend_few<TYPE, D, 1>(p, blockIdx.x - tiles, buf);
+    }
+}
+
+template <int TYPE, int D, int ROWS>
+__global__ __launch_bounds__(256) void join_few_kernel(const AttnParams p) {
+    join_parts<TYPE, D, ROWS, 128>(p, p.few, blockIdx.x);
+}
+
+template <int TYPE, int D>
+__global__ __launch_bounds__(256) void join_mixed_kernel(const AttnParams p) {
+    const int tiles = 2 * p.many.pieces * p.Hk;
+    if ((int)blockIdx.x < tiles) join_parts<TYPE, D, kTileRows, tile_keys(D)>(p, p.many, blockIdx.x);
+    else join_parts<TYPE, D, 16, 128>(p, p.few, blockIdx.x - tiles);
+}
+
+// The launch for a call: whether requests may have more than kFew rows, the rows of a tile of few (16 or 32), and the pieces aimed at over all KV heads.
+// Few rows, 768 workgroups at a time, bound by reading: 64 ragged requests of 64 heads with 768, 1024 and 2048 pieces 236, 228, 235 us, 8 of 32k on 128
+// heads 217, 204, 213, one of 4101 tokens 19.5, 19.8, 23.6.  Many rows, 512 at a time, bound by the matrix cores, where a last round of few workgroups
+// costs as much as a full one and parts more than whole tiles: three quarters of a round, since parts are rounded up (three pieces of
+// prompts on 16 heads of 256 with 384, 512 and 1024 pieces 184, 247, 252 us).
+constexpr int kPieces = 1024, kTilePieces = 384;
+
 struct AttnPlan {
-    int rows, pieces;
-    int64_t slot_bytes(int D) const { return (int64_t)rows * (D + 2) * 4; }
-    size_t bytes(int Hk, int D) const { return (size_t)(2 * (int64_t)pieces * Hk * slot_bytes(D)); }
+    bool mixed;
+    int rows, few, many;                                     // pieces a KV head
+    static size_t slots_bytes(int pieces, int rows, int Hk, int D) { return (size_t)2 * pieces * Hk * rows * (D + 2) * 4; }
+    size_t bytes(int Hk, int D) const { return slots_bytes(few, rows, Hk, D) + slots_bytes(many, kTileRows, Hk, D); }
 };
 
 static AttnPlan plan_attention(int64_t T, int B, int Hq, int Hk, int D, int max_new) {
-    const int G = Hq / Hk;
+    const int64_t rows = std::min<int64_t>(max_new, T) * (Hq / Hk);
     AttnPlan a;
-    const int64_t rows = (int64_t)max_new * G;
-    a.rows = rows > 64 ? kTileRows : rows <= 16 || D == 256 ? 16 : 32;
-    a.pieces = ((a.rows == kTileRows ? kTilePieces : kPieces) + Hk - 1) / Hk;
+    a.mixed = rows > kFew;
+    a.rows = a.mixed || rows <= 16 || D == 256 ? 16 : 32;
+    a.few = a.mixed && B == 1 ? 0 : (kPieces + Hk - 1) / Hk;
+    a.many = a.mixed ? (kTilePieces + Hk - 1) / Hk : 0;
     return a;
-}
-
-template <int TYPE, int D, int NQ>
-static void launch_rows(const AttnParams& p, hipStream_t st) {
-    const int64_t tiles = (int64_t)p.T * p.G / (16 * NQ) + p.B;
-    hipLaunchKernelGGL((attend_rows_kernel<TYPE, D, NQ>), dim3((unsigned)((tiles + p.pieces) * p.Hk)), dim3(256), 0, st, p);
-    if (p.pieces) hipLaunchKernelGGL((join_parts_kernel<TYPE, D, 16 * NQ, 128>), dim3((unsigned)(tiles * p.Hk)), dim3(256), 0, st, p);
 }
 
 template <int TYPE, int D>
 static void launch_attention(const AttnParams& p, const AttnPlan& a, hipStream_t st) {
-    if (a.rows == kTileRows) {
-        constexpr int KEYS = D == 256 ? 32 : 64;
-        const int64_t tiles = (int64_t)p.T * p.G / kTileRows + p.B;
-        hipLaunchKernelGGL((attend_tiles_kernel<TYPE, D, KEYS>), dim3((unsigned)((tiles + p.pieces) * p.Hk)), dim3(256), 0, st, p);
-        if (p.pieces) hipLaunchKernelGGL((join_parts_kernel<TYPE, D, kTileRows, KEYS>), dim3((unsigned)(tiles * p.Hk)), dim3(256), 0, st, p);
+    if (a.mixed) {
+        hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D>), dim3((unsigned)((p.many.most + p.few.most) * p.Hk)), dim3(256), 0, st, p);
+        const unsigned slots = 2 * (p.many.pieces + p.few.pieces) * p.Hk;
+        if (slots) hipLaunchKernelGGL((join_mixed_kernel<TYPE, D>), dim3(slots), dim3(256), 0, st, p);
         return;
     }
+    const dim3 grid((unsigned)(p.few.most * p.Hk)), join((unsigned)(2 * p.few.pieces * p.Hk));
     if constexpr (D < 256) {
-        if (a.rows == 32) return launch_rows<TYPE, D, 2>(p, st);
+        if (a.rows == 32) {
+            hipLaunchKernelGGL((attend_few_kernel<TYPE, D, 2>), grid, dim3(256), 0, st, p);
+            if (p.few.pieces) hipLaunchKernelGGL((join_few_kernel<TYPE, D, 32>), join, dim3(256), 0, st, p);
+            return;
+        }
     }
-    launch_rows<TYPE, D, 1>(p, st);
+    hipLaunchKernelGGL((attend_few_kernel<TYPE, D, 1>), grid, dim3(256), 0, st, p);
+    if (p.few.pieces) hipLaunchKernelGGL((join_few_kernel<TYPE, D, 16>), join, dim3(256), 0, st, p);
 }
 
 }  // namespace rtn
@@ -666,16 +753,26 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     if (q_stride % 8 || !rtn::aligned_to(dev_q, 16) || !rtn::aligned_to(dev_out, 16) || !rtn::aligned_to(dev_workspace, 16) ||
         !rtn::aligned_to(dev_block_table, 4) || !rtn::aligned_to(dev_seq_lens, 4) || !rtn::aligned_to(dev_query_start, 4))
         return RTN_ERR_ALIGN;
-    if ((tokens * (q_heads / cache->kv_heads) / 16 + n_requests) * cache->kv_heads >= 0x7FFFFFFF) return RTN_ERR_SHAPE;
     if (tokens == 0) return RTN_OK;
-    const rtn::AttnPlan a = rtn::plan_attention(tokens, n_requests, q_heads, cache->kv_heads, D, max_new);
-    const int64_t room = dev_workspace ? (int64_t)(workspace_nbytes / (size_t)(2 * cache->kv_heads * a.slot_bytes(D))) : 0;
+    const int Hk = cache->kv_heads, G = q_heads / Hk;
+    rtn::AttnPlan a = rtn::plan_attention(tokens, n_requests, q_heads, Hk, D, max_new);
+    // a smaller workspace than asked for: fewer pieces of either kind
+    auto room = [&](size_t bytes, int rows) { return (int)std::min<size_t>(bytes / rtn::AttnPlan::slots_bytes(1, rows, Hk, D), 1 << 20); };
+    size_t left = dev_workspace ? workspace_nbytes : 0;
+    a.many = std::min(a.many, room(left, rtn::kTileRows));
+    const size_t tiles_bytes = rtn::AttnPlan::slots_bytes(a.many, rtn::kTileRows, Hk, D);
+    a.few = std::min(a.few, room(left - tiles_bytes, a.rows));
+    // bounds on the pieces of a KV head: a request's last tile may be ragged, and each of its tiles have one part more than its share
+    const int64_t rows = tokens * G;
+    const int64_t few_tiles = std::min(rows / a.rows + n_requests, a.mixed ? (int64_t)n_requests * (rtn::kFew / a.rows) : rows);
+    const int64_t many_tiles = a.mixed ? rows / rtn::kTileRows + std::min<int64_t>(n_requests, rows / rtn::kFew) : 0;
+    if ((few_tiles + a.few + many_tiles + a.many) * Hk >= 0x7FFFFFFF) return RTN_ERR_SHAPE;
     const float log2e = 1.4426950408889634f;
+    float* const ws = static_cast<float*>(dev_workspace);
     const rtn::AttnParams p = {dev_q, cache->dev_k, cache->dev_v, dev_out, dev_block_table, dev_seq_lens, dev_query_start, q_stride, cache->page_stride,
                                cache->head_stride, cache->token_stride, table_stride, (int)cache->pages, rtn::log2_of(cache->page_size), max_blocks,
-                               n_requests, (int)tokens, q_heads, cache->kv_heads, q_heads / cache->kv_heads, window, scale * log2e, softcap,
-                               softcap > 0.f ? scale / softcap : 0.f, softcap * log2e, static_cast<float*>(dev_workspace),
-                               (int)(room < a.pieces ? room : a.pieces)};
+                               n_requests, (int)tokens, q_heads, Hk, G, window, scale * log2e, softcap, softcap > 0.f ? scale / softcap : 0.f,
+                               softcap * log2e, a.mixed ? rtn::kFew : 0x7FFFFFFF, {ws + tiles_bytes / 4, a.few, (int)(few_tiles + a.few)}, {ws, a.many, (int)(many_tiles + a.many)}};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == RTN_TYPE_F16) {
         if (D == 64) rtn::launch_attention<RTN_TYPE_F16, 64>(p, a, s);
