@@ -181,7 +181,7 @@ __device__ __forceinline__ void clear_padding(const AttnParams& p, int D) {
 }
 
 // The parts of a tile's keys, brought to their common maximum and added up.  The workgroups of a tile, as many as it has parts, share its rows.
-// D / 4 threads take a row's sums of a part: 1024 / D parts or, of fewer parts, several rows at a time.
+// D / 4 threads take a row's sums of a part: 1024 / D rows at a time or, of fewer rows, several parts of them.
 template <int TYPE, int D, int ROWS, int KEYS>
 __device__ __forceinline__ void join_parts(const AttnParams& p, const AttnKind& kind, int block) {
     typedef typename Elem<TYPE>::one T;
@@ -194,9 +194,9 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, const AttnKind& 
     if (!find_piece<ROWS, KEYS, true>(p, kind.pieces, block / p.Hk, &w) || w.parts == 1) return;
     const float *const po = partial_sums(p, kind, head, w.slot, ROWS, D) + lane * 4, *const pm = partial_stats(p, kind, head, w.slot, ROWS, D);
     const int r0 = w.rows * w.part / w.parts, r1 = w.rows * (w.part + 1) / w.parts;
-    int by_parts = 1;                                        // groups that share a row
-    while (by_parts < GROUPS && by_parts < w.parts) by_parts *= 2;
-    const int at_once = GROUPS / by_parts, first = group & (by_parts - 1);
+    int at_once = 1;                                         // rows; the other groups share a row's parts
+    while (at_once < GROUPS && at_once < r1 - r0) at_once *= 2;
+    const int by_parts = GROUPS / at_once, first = group & (by_parts - 1);
     for (int r = r0 + group / by_parts; r < r1 + at_once - 1; r += at_once) {      // (as many turns for all groups)
         float4_t acc = {0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
@@ -242,6 +242,10 @@ __device__ __forceinline__ void wave_sync() {
     __builtin_amdgcn_wave_barrier();
     __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
+
+// Where a 16-byte piece of a staged key row is: 16 rows, as many as the lanes that read at once, in different banks.
+template <int D>
+__device__ __forceinline__ int k_swizzle(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
 
 // Few rows: 16 NQ of them a workgroup, whose four wavefronts take blocks of 32 keys in turn, each with a softmax of its own until they join
 // at the end.  Bound by the reading of K and V, which go through LDS one after the other, 8 KiB that only its wavefront touches (D = 128), so that
@@ -317,7 +321,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
 #pragma unroll
         for (int j = 0; j < VI; ++j) {
             const int key = (j * 64 + lane) / CH, piece = lane % CH;
-            *reinterpret_cast<u32x4_t*>(vb + key * (D * 2) + (piece ^ (key & 7)) * 16) = k[j];
+            *reinterpret_cast<u32x4_t*>(vb + key * (D * 2) + (piece ^ k_swizzle<D>(key)) * 16) = k[j];
         }
         wave_sync();
         float4_t s[NQ][2];
@@ -327,7 +331,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
         for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int t = 0; t < KS; ++t) {
-                const T8 a = *reinterpret_cast<const T8*>(vb + (16 * h + col) * (D * 2) + ((4 * t + grp) ^ (col & 7)) * 16);
+                const T8 a = *reinterpret_cast<const T8*>(vb + (16 * h + col) * (D * 2) + ((4 * t + grp) ^ k_swizzle<D>(col)) * 16);
 #pragma unroll
                 for (int n = 0; n < NQ; ++n) s[n][h] = Elem<TYPE>::mfma16(a, q[n][t], s[n][h]);
             }
@@ -457,7 +461,7 @@ __device__ __forceinline__ void landed() {
 
 // Many rows: 128 of them a workgroup, 32 a wavefront, over blocks of KEYS keys that are staged in LDS, the next block on its way while one is
 // worked on.  Bound by the matrix cores and, about as much, by the exponentials: two workgroups share a compute unit, so that one's
-// products run beside the other's softmax.  Rows of a staged block are permuted by 16-byte pieces (K: by the key's last three
+// products run beside the other's softmax.  Rows of a staged block are permuted by 16-byte pieces (K: by the key's last four
 // bits; V: four pieces at a time by its last two, or, two rows of 64 lying side by side, the second of them), which spreads what the matrix operands read over all banks; the loads into LDS, whose
 // destinations are in lane order, take their sources permuted instead.
 __device__ __align__(16) uint32_t attention_zeros[4];        // what a key outside the request has for V
@@ -502,12 +506,12 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
     const int any0 = p.window ? pos_lo - p.window + 1 : 0, any1 = wrow < w.rows ? pos_hi + 1 : 0;
 
     // sources of a wavefront's loads: rows MINE wave .. of a block, a lane's piece permuted back
-    uint32_t koff[LOADS], voff[LOADS];                       // in elements
+    uint32_t koff[LOADS], voff[LOADS];                       // in bytes
 #pragma unroll
     for (int j = 0; j < LOADS; ++j) {
         const int r = j * PER + lane / CH, rr = MINE * wave + r, piece = lane % CH;
-        koff[j] = r * (uint32_t)p.token_stride + (piece ^ (rr & 7)) * 8;
-        voff[j] = r * (uint32_t)p.token_stride + (piece ^ (D == 64 ? (rr & 2) * 2 : (rr & 3) * 4)) * 8;
+        koff[j] = (r * (uint32_t)p.token_stride + (piece ^ k_swizzle<D>(rr)) * 8) * sizeof(T);
+        voff[j] = (r * (uint32_t)p.token_stride + (piece ^ (D == 64 ? (rr & 2) * 2 : (rr & 3) * 4)) * 8) * sizeof(T);
     }
     int ids = 0;
     auto stage = [&](int block, uint8_t* kb, uint8_t* vb) {
@@ -518,19 +522,22 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
         }
         const int64_t page = __builtin_amdgcn_readlane(ids, i & 63);
         const int64_t off = page * p.page_stride + head * p.head_stride + (int64_t)(key & (ps - 1)) * p.token_stride;
-        const T *const kp = static_cast<const T*>(p.k) + off, *const vp = static_cast<const T*>(p.v) + off;
-        const bool edge = key < w.kv0 || key + MINE > w.kv1;
+        const char *const kp = reinterpret_cast<const char*>(static_cast<const T*>(p.k) + off), *const vp = reinterpret_cast<const char*>(static_cast<const T*>(p.v) + off);
+        auto to_lds = [&](const char* from, uint8_t* to, int j) {
+            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)from,
+                                             (__attribute__((address_space(3))) void*)(to + (MINE * wave + j * PER) * D * 2), 16, 0, 0);
+        };
 #pragma unroll
-        for (int j = 0; j < LOADS; ++j) {
-            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)(kp + koff[j]),
-                                             (__attribute__((address_space(3))) void*)(kb + (MINE * wave + j * PER) * D * 2), 16, 0, 0);
-            const T* src = vp + voff[j];
-            if (edge) {                                      // slots without a token of the request may hold anything
-                const int k = key + j * PER + lane / CH;
-                if (k < w.kv0 || k >= w.kv1) src = reinterpret_cast<const T*>(attention_zeros);
+        for (int j = 0; j < LOADS; ++j) to_lds(kp + koff[j], kb, j);
+        if (key >= w.kv0 && key + MINE <= w.kv1) {
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) to_lds(vp + voff[j], vb, j);
+        } else {                                             // slots without a token of the request may hold anything
+#pragma unroll
+            for (int j = 0; j < LOADS; ++j) {
+                const int at = key + j * PER + lane / CH;
+                to_lds(at < w.kv0 || at >= w.kv1 ? reinterpret_cast<const char*>(attention_zeros) : vp + voff[j], vb, j);
             }
-            __builtin_amdgcn_global_load_lds((__attribute__((address_space(1))) void*)src,
-                                             (__attribute__((address_space(3))) void*)(vb + (MINE * wave + j * PER) * D * 2), 16, 0, 0);
         }
     };
     auto work = [&](int block, const uint8_t* kb, const uint8_t* vb) {
@@ -538,15 +545,29 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
         if (k0 >= any1 || k0 + KEYS <= any0) return;
         float16_t s[KT];
 #pragma unroll
-        for (int h = 0; h < KT; ++h) {
+        for (int h = 0; h < KT; ++h)
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[h][j] = 0.f;
+        // The operands are read four products ahead, and the wavefront in its products goes before the other workgroup's in its softmax (the two, with
+        // the order of the second product below: 2000 tokens over 30001 2237 -> 2140 us, 4096 tokens of a prompt 183 -> 174).
+        constexpr int kAhead = 4;
+        __builtin_amdgcn_s_setprio(1);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int t = 0; t < KS; ++t) {
-                const T8 a = *reinterpret_cast<const T8*>(kb + (32 * h + col) * D * 2 + (((2 * t + hi) ^ (col & 7)) * 16));
+        for (int t = 0; t < KS; ++t)
+#pragma unroll
+            for (int h = 0; h < KT; ++h) {
+                const T8 a = *reinterpret_cast<const T8*>(kb + (32 * h + col) * D * 2 + (((2 * t + hi) ^ k_swizzle<D>(col)) * 16));
                 s[h] = Elem<TYPE>::mfma32(a, q[t], s[h]);
             }
+        __builtin_amdgcn_sched_group_barrier(0x100, kAhead, 0);
+#pragma unroll
+        for (int i = 0; i < KS * KT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            if (i < KS * KT - kAhead) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
+        __builtin_amdgcn_sched_barrier(0);
+        __builtin_amdgcn_s_setprio(0);
         float scale = p.scale2;
         if (p.cap > 0.f) {
             scale = 1.f;
@@ -582,19 +603,18 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
                 for (int j = 0; j < 16; ++j) o[t][j] *= back;
         }
         const float base = m == -INFINITY ? 0.f : m;
-        T8 pt[KT * 2];
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int h = 0; h < KT; ++h)
+        for (int h = 0; h < KT * 2; ++h) {
+            T8 pt;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                const float x = exp2_of(fmaf(s[h][j], scale, -base));
+            for (int j = 0; j < 8; ++j) {
+                const float x = exp2_of(fmaf(s[h >> 1][8 * (h & 1) + j], scale, -base));
                 l += x;
-                pt[2 * h + (j >> 3)][j & 7] = (T)x;          // (the weight of V in the element type: half an ulp of it, as much as the result's own rounding)
+                pt[j] = (T)x;                                // (the weight of V in the element type: half an ulp of it, as much as the result's own rounding)
             }
 #pragma unroll
-        for (int t = 0; t < DT; ++t)
-#pragma unroll
-            for (int h = 0; h < KT * 2; ++h) {
+            for (int t = 0; t < DT; ++t) {
                 union { T8 v; short4_t s[2]; } a;
 #pragma unroll
                 for (int x = 0; x < 2; ++x) {
@@ -603,8 +623,22 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
                     a.s[x] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
                         (__attribute__((address_space(3))) short4_t*)(vb + key * D * 2 + piece * 16 + (i & 1) * 8));
                 }
-                o[t] = Elem<TYPE>::mfma32(a.v, pt[h], o[t]);
+                o[t] = Elem<TYPE>::mfma32(a.v, pt, o[t]);
             }
+        }
+        // the first weights behind the first operands; then a product, two operand reads and a share of the other weights at a time
+        constexpr int N = 2 * KT * DT, REST = (56 * KT - 28 + N - DT - 1) / (N - DT);
+        __builtin_amdgcn_sched_group_barrier(0x100, 2 * DT, 1);
+        __builtin_amdgcn_sched_group_barrier(0x002, 28, 1);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+            if (i < N - DT) {
+                __builtin_amdgcn_sched_group_barrier(0x100, 2, 1);
+                __builtin_amdgcn_sched_group_barrier(0x002, REST, 1);
+            }
+        }
+        __builtin_amdgcn_sched_barrier(0);
     };
 
     // (the queries are waited for here: in the loop that would be a wait for the loads into LDS as well)
