@@ -343,10 +343,10 @@ typedef struct {
  *                     -1 from query_start[n_requests] on
  *   dev_free_count_out, dev_status   out  int32 [1]
  * status: 0, or what does not fit, as a sum of 1 (pages), 2 (a row of the table), 4 (max_tokens), 8 (a length or count out of range:
- * cached_lens, free_count, more pages back than the pool holds).  Then nothing happens: lengths and count stay, query_start is 0,
+ * cached_lens, free_count, or more pages back than the stack has entries).  Then nothing happens: lengths and count stay, query_start is 0,
  * positions and slots -1, table and stack are untouched.
  * dev_seq_lens may be dev_cached_lens and dev_free_count_out may be dev_free_count, as a loop of replays wants it; no other buffers may
- * overlap.  n_requests 1 .. 4096, max_tokens and pool below 2^30. */
+ * overlap.  n_requests 1 .. 4096, max_tokens below 2^30, pool up to 2^27. */
 rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev_cached_lens, int n_requests, int page_size,
                           int32_t* dev_block_table, int64_t table_stride, int max_blocks,
                           int32_t* dev_free_pages, int64_t pool, const int32_t* dev_free_count,

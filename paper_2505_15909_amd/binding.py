@@ -118,7 +118,7 @@ _lib = _load()
 
 
 def _load_native():
-    """The small calls in native code (csrc/rtn_native.cpp), or None where they were not built; without them a call takes 5.3 us of host time
+    """The small calls in native code (csrc/rtn_native.cpp), or None where they were not built; without them a linear call takes 5.3 us of host time
     instead of 3.1.  They read PyTorch's own objects, so a module compiled for another PyTorch or Python is left alone."""
     if not os.path.exists(os.path.join(os.path.dirname(__file__), "_native.so")):
         return None
@@ -131,7 +131,8 @@ def _load_native():
     if built_for != here:
         warnings.warn(f"the binding's native calls were compiled for {built_for}, this is {here}: build the library again", RuntimeWarning)
         return None
-    module.bind(C.cast(_lib.rtn_linear, C.c_void_p).value, C.cast(_lib.rtn_linear_asym, C.c_void_p).value)
+    module.bind(*(C.cast(f, C.c_void_p).value for f in (_lib.rtn_linear, _lib.rtn_linear_asym, _lib.rtn_cache_plan, _lib.rtn_rope_cache,
+                                                        _lib.rtn_paged_attention)))
     return module
 
 
@@ -461,7 +462,7 @@ class PagedCache:
         self.dtype, self.device = k.dtype, k.device
         self.desc = rtn_kv_cache(k.data_ptr(), v.data_ptr(), self.pages, self.page_size, self.kv_heads, self.head_dim, _TYPES[k.dtype],
                                  k.stride(0), k.stride(1), k.stride(2))
-        self._ref = C.byref(self.desc)
+        self._ref, self._address = C.byref(self.desc), C.addressof(self.desc)
 
 
 class CachePlan(collections.namedtuple("CachePlan", "seq_lens query_start positions slots free_count status")):
@@ -494,6 +495,11 @@ def rtn_cache_plan(step: torch.Tensor, cached_lens: torch.Tensor, block_table: t
     """A step's block tables, slots and positions: request b appends step[b] tokens to its cached_lens[b] (or ends, step[b] < 0), with pages
     off the stack free_pages[:free_count].  block_table [requests, blocks] and free_pages are updated.  out.seq_lens may be cached_lens and
     out.free_count free_count, for a loop of replays.  out.status says what did not fit (0: nothing), and then nothing has changed."""
+    if _native is not None and out is not None:
+        st = _native.cache_plan(step, cached_lens, block_table, free_pages, free_count, page_size, max_tokens, out)
+        if st is not None:
+            _check(st, "rtn_cache_plan")
+            return out
     _dev_int32(step, "step")
     B = step.shape[0]
     _dev_int32(cached_lens, "cached_lens", B)
@@ -518,6 +524,11 @@ def rtn_rope_cache(qkv: torch.Tensor, q_heads: int, rope: torch.Tensor, position
                    out: torch.Tensor = None) -> torch.Tensor:
     """qkv [tokens, (q_heads + 2 kv_heads) * head_dim], the QKV projection's output -> queries [tokens, q_heads, head_dim], normed (where weights
     are given) and rotated; keys, the same way, and values go to the cache's slots.  rope fp32 [positions, rotary_dim]: cosines, then sines."""
+    if _native is not None and out is not None:
+        st = _native.rope_cache(qkv, q_heads, rope, positions, slots, cache._address, q_norm, k_norm, eps, interleaved, out)
+        if st is not None:
+            _check(st, "rtn_rope_cache")
+            return out
     D, Hk, T = cache.head_dim, cache.kv_heads, qkv.shape[0]
     if not (qkv.is_cuda and qkv.dtype is cache.dtype and qkv.dim() == 2 and qkv.shape[1] == (q_heads + 2 * Hk) * D and qkv.stride(1) == 1):
         raise ValueError(f"qkv must be a CUDA matrix of the cache's type with {(q_heads + 2 * Hk) * D} contiguous columns")
@@ -547,6 +558,11 @@ def rtn_paged_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.T
                         workspace: torch.Tensor = None) -> torch.Tensor:
     """q [tokens, q_heads, head_dim], request b's new tokens being rows query_start[b] .. query_start[b + 1] - 1 and the last of its seq_lens[b]
     tokens in the cache -> attention output of the same shape.  max_new: a bound on the new tokens of one request."""
+    if _native is not None and out is not None and workspace is not None:
+        st = _native.paged_attention(q, cache._address, block_table, seq_lens, query_start, max_new, scale, softcap, window, out, workspace)
+        if st is not None:
+            _check(st, "rtn_paged_attention")
+            return out
     T, Hq, D = q.shape
     if not (q.is_cuda and q.dtype is cache.dtype and D == cache.head_dim and q.stride(2) == 1 and (q.stride(1) == D or Hq == 1)):
         raise ValueError("q must be a CUDA tensor [tokens, q_heads, head_dim] of the cache's type, contiguous within a token")

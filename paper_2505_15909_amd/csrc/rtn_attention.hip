@@ -58,7 +58,7 @@ struct Piece {
 // thread's (one, up to 256 of them) read once.  `no` counts the pieces, or, JOIN, those of split requests alone.  All 256 threads call it.
 template <int ROWS, int KEYS, bool JOIN>
 __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int no, Piece* out) {
-    __shared__ int64_t totals[4];
+    __shared__ float totals[4];
     __shared__ int sums[4][2], found[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (p.B + 255) / 256, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
@@ -81,17 +81,17 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
     auto request = [&](int b) { return b == b0 ? own : read(b); };
     int c = 0x7FFFFFFF;
     if (pieces) {
-        int64_t total = 0;
+        float total = 0.f;
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
-            total += (int64_t)r.tiles * r.blocks;
+            total += (float)r.tiles * (float)r.blocks;
         }
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) total += __shfl_xor((long long)total, d);
-        if (lane == 0) totals[wave] = total;
+        total = wave_scan(total);
+        if (lane == 63) totals[wave] = total;
         __syncthreads();
-        total = totals[0] + totals[1] + totals[2] + totals[3];
-        c = (int)min((int64_t)0x7FFFFFFF, max((int64_t)1, (total + pieces - 1) / pieces));
+        // (not below the exact share, for the room that there is for partial results: the sums' rounding is less than 2^-10)
+        total = ((totals[0] + totals[1]) + (totals[2] + totals[3])) * (1.0f + 0x1p-10f);
+        c = (int)fminf(0x1p30f, fmaxf(1.f, ceilf(total / (float)pieces)));
     }
     auto parts_of = [&](int blocks) { return max(1, (int)(((int64_t)blocks + c - 1) / c)); };
     int mine[2] = {0, 0};                                    // pieces, and those of split requests
@@ -101,15 +101,7 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
         mine[0] += r.tiles * parts;
         mine[1] += parts > 1 ? r.tiles * parts : 0;
     }
-    int incl[2] = {mine[0], mine[1]};
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            const int o = __shfl_up(incl[k], d);
-            if (lane >= d) incl[k] += o;
-        }
-    }
+    const int incl[2] = {wave_scan(mine[0]), wave_scan(mine[1])};
     if (lane == 63) {
         sums[wave][0] = incl[0];
         sums[wave][1] = incl[1];

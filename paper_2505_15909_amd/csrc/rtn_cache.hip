@@ -56,64 +56,72 @@ __device__ __forceinline__ Request read_request(const PlanParams& p, int b) {
 
 __global__ __launch_bounds__(1024) void cache_plan_kernel(const PlanParams p) {
     extern __shared__ int lds[];
+    __shared__ int part[16][4];
+    __shared__ float large[16][3];
     int *const ends = lds, *const pops = ends + p.B, *const frees = pops + p.B, *const cached = frees + p.B;
-    int64_t* const part = reinterpret_cast<int64_t*>(cached + p.B);
     const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6, waves = threads >> 6;
     const int count = *p.count;
 
-    // each thread's requests, then the sums before it: within the wavefront, then over the wavefronts (64 bits: lengths may add up to more)
+    // Each thread's requests, then the sums before it: within the wavefront, then over the wavefronts.  32 bits hold every sum that is used:
+    // one that they do not hold is seen by its sum in fp32, and is more than there can be.
     const int per = (p.B + threads - 1) / threads, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
-    int64_t sum[3] = {0, 0, 0};
+    Request own = {};
+    if (b0 < b1) own = read_request(p, b0);
+    auto request = [&](int b) { return b == b0 ? own : read_request(p, b); };
+    uint32_t sum[3] = {0, 0, 0};
+    float about[3] = {0.f, 0.f, 0.f};
     int flags = 0;
     for (int b = b0; b < b1; ++b) {
-        const Request r = read_request(p, b);
+        const Request r = request(b);
         sum[0] += r.tokens;
         sum[1] += r.need;
         sum[2] += r.freed;
+        about[0] += (float)r.tokens;
+        about[1] += (float)r.need;
+        about[2] += (float)r.freed;
         flags |= r.flags;
     }
-    int64_t before[3], total[3];
+    uint32_t before[3], total[3] = {0, 0, 0};
+    float most[3] = {0.f, 0.f, 0.f};
+    flags = (__any(flags & 1) ? 1 : 0) | (__any(flags & 2) ? 2 : 0) | (__any(flags & 4) ? 4 : 0) | (__any(flags & 8) ? 8 : 0);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
-        int64_t s = sum[k];
-#pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int64_t o = __shfl_up((long long)s, d);
-            if (lane >= d) s += o;
-        }
+        const uint32_t s = wave_scan(sum[k]);
+        const float f = wave_scan(about[k]);
         before[k] = s - sum[k];
-        if (lane == 63) part[wave * 4 + k] = s;
+        if (lane == 63) {
+            part[wave][k] = s;
+            large[wave][k] = f;
+        }
     }
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) flags |= __shfl_xor(flags, d);
-    if (lane == 0) part[wave * 4 + 3] = flags;
+    if (lane == 63) part[wave][3] = flags;
     __syncthreads();
-#pragma unroll
-    for (int k = 0; k < 3; ++k) total[k] = 0;
     flags = 0;
     for (int w = 0; w < waves; ++w) {
 #pragma unroll
         for (int k = 0; k < 3; ++k) {
-            if (w < wave) before[k] += part[w * 4 + k];
-            total[k] += part[w * 4 + k];
+            if (w < wave) before[k] += part[w][k];
+            total[k] += part[w][k];
+            most[k] += large[w][k];
         }
-        flags |= (int)part[w * 4 + 3];
+        flags |= part[w][3];
     }
-    const int64_t left = count + total[2] - total[1];
-    if (count < 0 || count > p.pool || left > p.pool) flags |= 8;
-    if (left < 0) flags |= 1;
-    if (total[0] > p.max_tokens) flags |= 4;
+    const int64_t left = (int64_t)count + total[2] - total[1];
+    if (count < 0 || count > p.pool || most[2] > 0x1p29f || total[2] > (uint64_t)p.pool) flags |= 8;
+    else if (most[1] > 0x1p30f || left < 0) flags |= 1;      // (count and what comes back are 2^28 at most)
+    else if (left > p.pool) flags |= 8;
+    if (most[0] > 0x1.01p30f || total[0] > (uint32_t)p.max_tokens) flags |= 4;
 
     // (where flags are set, the sums are not used)
     for (int b = b0; b < b1; ++b) {
-        const Request r = read_request(p, b);
+        const Request r = request(b);
         before[0] += r.tokens;
         before[1] += r.need;
         before[2] += r.freed;
         ends[b] = (int)before[0];
         pops[b] = (int)before[1];
         frees[b] = (int)before[2];
-        cached[b] = p.cached[b];
+        cached[b] = r.cached;
     }
     __syncthreads();
 
@@ -252,7 +260,7 @@ extern "C" rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev
         (max_tokens > 0 && (!dev_positions || !dev_slots)) || !dev_free_count_out || !dev_status)
         return RTN_ERR_NULL;
     if (n_requests < 1 || n_requests > 4096 || !rtn::page_size_valid(page_size) || max_blocks < 1 || max_blocks > (1 << 30) / page_size ||
-        table_stride < max_blocks || pool < 1 || pool >= (int64_t)1 << 30 || max_tokens < 0 || max_tokens >= (int64_t)1 << 30)
+        table_stride < max_blocks || pool < 1 || pool > 1 << 27 || max_tokens < 0 || max_tokens >= (int64_t)1 << 30)
         return RTN_ERR_SHAPE;
     for (const void* q : {(const void*)dev_step, (const void*)dev_cached_lens, (const void*)dev_block_table, (const void*)dev_free_pages,
                           (const void*)dev_free_count, (const void*)dev_seq_lens, (const void*)dev_query_start, (const void*)dev_positions,
@@ -265,8 +273,8 @@ extern "C" rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev
     const int threads = in_place ? 1024 : 256;
     const int64_t work = max_tokens > n_requests ? max_tokens : n_requests;
     const unsigned blocks = in_place ? 1 : (unsigned)(work < 256 * 64 ? (work + 255) / 256 : 64);
-    const size_t lds = (size_t)n_requests * 16 + 16 * 4 * sizeof(int64_t);
-    if (lds > 65536 && hipFuncSetAttribute(reinterpret_cast<const void*>(&rtn::cache_plan_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
+    const size_t lds = (size_t)n_requests * 16;
+    if (lds > 61440 && hipFuncSetAttribute(reinterpret_cast<const void*>(&rtn::cache_plan_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) != hipSuccess)
         return RTN_ERR_HIP;
     hipLaunchKernelGGL(rtn::cache_plan_kernel, dim3(blocks), dim3(threads), lds, static_cast<hipStream_t>(stream), p);
     return hipGetLastError() == hipSuccess ? RTN_OK : RTN_ERR_HIP;

@@ -32,6 +32,24 @@ template <> struct Elem<RTN_TYPE_BF16> {
     static __device__ __forceinline__ float16_t mfma32(x8 a, x8 b, float16_t c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
 };
 
+// Sums over the lanes before and including this one: four shifts within rows of 16, then the rows' last sums to the rows behind.  (Six vector
+// instructions; by way of LDS, as shuffles go, a scan takes half a microsecond of a call of a few.)
+template <int CTRL, int ROWS, typename T>
+__device__ __forceinline__ T from_lane(T x) {                // zero where there is no such lane
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), CTRL, ROWS, 0xF, false));
+}
+
+template <typename T>
+__device__ __forceinline__ T wave_scan(T x) {
+    x += from_lane<0x111, 0xF>(x);                           // row_shr:1, 2, 4, 8
+    x += from_lane<0x112, 0xF>(x);
+    x += from_lane<0x114, 0xF>(x);
+    x += from_lane<0x118, 0xF>(x);
+    x += from_lane<0x142, 0xA>(x);                           // row_bcast:15 into rows 1 and 3, row_bcast:31 into 2 and 3
+    x += from_lane<0x143, 0xC>(x);
+    return x;
+}
+
 // Host-side checks.
 inline bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
