@@ -384,7 +384,7 @@ rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_t qkv_strid
  *   dev_out        out  [tokens, q_heads, head_dim]
  *   dev_workspace  scratch, rtn_paged_attention_workspace_nbytes() bytes; with less or NULL long requests are not split over
  *                  workgroups (slower, not an error); contents undefined before and after; calls that overlap in time need distinct ones
- * q_heads a multiple of kv_heads, up to 64 times as many; tokens 0 .. 2^24; n_requests 1 .. 65536.  The same inputs with the same
+ * q_heads a multiple of kv_heads, up to 64 times as many; tokens 0 .. 2^20; n_requests 1 .. 65536.  The same inputs with the same
  * workspace size give the same bits. */
 size_t rtn_paged_attention_workspace_nbytes(int64_t tokens, int n_requests, int q_heads, const rtn_kv_cache* cache, int max_new);
 rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int64_t q_stride, int q_heads, const rtn_kv_cache* cache,

@@ -16,12 +16,13 @@ namespace rtn {
 
 // Requests of up to kFew rows go to the workgroups for few rows, longer ones to those for many (kTileRows).
 constexpr int kFew = 64, kTileRows = 128;
+constexpr int kFewKeys = 128;                                // keys of a step of the four wavefronts of a workgroup for few rows
 
 // One of the two kinds of workgroups in a launch.  `pieces` a KV head are aimed at (0: no request is split), and a head has room for twice as many
 // partial results, [Hk][2 pieces][rows][D] sums and, behind them, [Hk][2 pieces][rows][2] maxima and sums of weights.
 struct AttnKind {
     float* partial;
-    int pieces, most;                                        // most: a bound on the pieces of a KV head
+    int pieces, most, slots;                                 // bounds on the pieces of a KV head and on those of split requests
 };
 
 struct AttnParams {
@@ -31,9 +32,12 @@ struct AttnParams {
     int64_t q_stride, page_stride, head_stride, token_stride, table_stride;
     int pages, shift, max_blocks, B, T, Hq, Hk, G, window;
     float scale2, cap, cap_in, cap_out;                      // scale log2 e; softcap: cap_out tanh(cap_in q.k), cap_out = softcap log2 e
+    uint32_t g_inv, g_one;                                   // row -> token is umulhi(row, g_inv) + (row & g_one): exact below 2^26 rows and G <= 64
     int few_rows;                                            // kFew, or no bound where the call's requests are all taken to have few
     AttnKind few, many;
 };
+
+__device__ __forceinline__ int token_of(const AttnParams& p, int row) { return (int)(__umulhi((uint32_t)row, p.g_inv) + ((uint32_t)row & p.g_one)); }
 
 // exp2 of scores: the softmax is taken to base 2, with log2 e in the scale
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -76,11 +80,32 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
         if (p.window) r.blocks = (int)min((int64_t)r.blocks, ((int64_t)p.window + ROWS / p.G + 1 + KEYS - 1) / KEYS + 1);
         return r;
     };
-    Request own = {};
-    if (b0 < b1) own = read(b0);
-    auto request = [&](int b) { return b == b0 ? own : read(b); };
-    int c = 0x7FFFFFFF;
-    if (pieces) {
+    auto shares = [&](float total) {
+        // (not below the exact share, for the room that there is for partial results: the sums' rounding is less than 2^-10)
+        return pieces ? (int)fminf(0x1p30f, fmaxf(1.f, ceilf(total * (1.0f + 0x1p-10f) / (float)pieces))) : 1 << 30;
+    };
+    int c, local, most, slot, n, seq;
+    auto parts_of = [&](int blocks) { return max(1, (int)(((uint32_t)blocks + c - 1) / c)); };      // (up to 2^26 blocks)
+    if (p.B <= 64) {                                         // a lane a request: each wavefront by itself, without LDS
+        Request r = {};
+        if (lane < p.B) r = read(lane);
+        c = shares(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan((float)r.tiles * (float)r.blocks)), 63)));
+        const int parts = parts_of(r.blocks), have = r.tiles * parts, slots = parts > 1 ? have : 0;
+        const int slots_before = wave_scan(slots) - slots, before = JOIN ? slots_before : wave_scan(have) - have;
+        const uint64_t hit = __ballot(no >= before && no < before + (JOIN ? slots : have));
+        if (hit == 0) return false;
+        const int b = __builtin_ctzll(hit);
+        out->b = b;
+        local = no - __builtin_amdgcn_readlane(before, b);
+        slot = __builtin_amdgcn_readlane(slots_before, b);
+        most = __builtin_amdgcn_readlane(parts, b);
+        out->tok0 = __builtin_amdgcn_readlane(r.tok0, b);
+        n = __builtin_amdgcn_readlane(r.n, b);
+        seq = __builtin_amdgcn_readlane(r.seq, b);
+    } else {
+        Request own = {};
+        if (b0 < b1) own = read(b0);
+        auto request = [&](int b) { return b == b0 ? own : read(b); };
         float total = 0.f;
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
@@ -89,68 +114,69 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
         total = wave_scan(total);
         if (lane == 63) totals[wave] = total;
         __syncthreads();
-        // (not below the exact share, for the room that there is for partial results: the sums' rounding is less than 2^-10)
-        total = ((totals[0] + totals[1]) + (totals[2] + totals[3])) * (1.0f + 0x1p-10f);
-        c = (int)fminf(0x1p30f, fmaxf(1.f, ceilf(total / (float)pieces)));
-    }
-    auto parts_of = [&](int blocks) { return max(1, (int)(((int64_t)blocks + c - 1) / c)); };
-    int mine[2] = {0, 0};                                    // pieces, and those of split requests
-    for (int b = b0; b < b1; ++b) {
-        const Request r = request(b);
-        const int parts = parts_of(r.blocks);
-        mine[0] += r.tiles * parts;
-        mine[1] += parts > 1 ? r.tiles * parts : 0;
-    }
-    const int incl[2] = {wave_scan(mine[0]), wave_scan(mine[1])};
-    if (lane == 63) {
-        sums[wave][0] = incl[0];
-        sums[wave][1] = incl[1];
-    }
-    if (tid == 0) found[0] = -1;
-    __syncthreads();
-    int before = incl[0] - mine[0], slot = incl[1] - mine[1];
-    for (int w = 0; w < wave; ++w) {
-        before += sums[w][0];
-        slot += sums[w][1];
-    }
-    if (JOIN) before = slot;
-    if (no >= before && no < before + mine[JOIN ? 1 : 0]) {
+        c = shares((totals[0] + totals[1]) + (totals[2] + totals[3]));
+        int mine[2] = {0, 0};                                // pieces, and those of split requests
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
-            const int parts = parts_of(r.blocks), slots = parts > 1 ? r.tiles * parts : 0, have = JOIN ? slots : r.tiles * parts;
-            if (no < before + have) {
-                found[0] = b;
-                found[1] = no - before;
-                found[2] = slot;
-                found[3] = parts;
-                found[4] = r.tok0;
-                found[5] = r.n;
-                found[6] = r.seq;
-                break;
-            }
-            before += have;
-            slot += slots;
+            const int parts = parts_of(r.blocks);
+            mine[0] += r.tiles * parts;
+            mine[1] += parts > 1 ? r.tiles * parts : 0;
         }
+        const int incl[2] = {wave_scan(mine[0]), wave_scan(mine[1])};
+        if (lane == 63) {
+            sums[wave][0] = incl[0];
+            sums[wave][1] = incl[1];
+        }
+        if (tid == 0) found[0] = -1;
+        __syncthreads();
+        int before = incl[0] - mine[0], slots_before = incl[1] - mine[1];
+        for (int w = 0; w < wave; ++w) {
+            before += sums[w][0];
+            slots_before += sums[w][1];
+        }
+        if (JOIN) before = slots_before;
+        if (no >= before && no < before + mine[JOIN ? 1 : 0]) {
+            for (int b = b0; b < b1; ++b) {
+                const Request r = request(b);
+                const int parts = parts_of(r.blocks), slots = parts > 1 ? r.tiles * parts : 0, have = JOIN ? slots : r.tiles * parts;
+                if (no < before + have) {
+                    found[0] = b;
+                    found[1] = no - before;
+                    found[2] = slots_before;
+                    found[3] = parts;
+                    found[4] = r.tok0;
+                    found[5] = r.n;
+                    found[6] = r.seq;
+                    break;
+                }
+                before += have;
+                slots_before += slots;
+            }
+        }
+        __syncthreads();
+        out->b = __builtin_amdgcn_readfirstlane(found[0]);
+        if (out->b < 0) return false;
+        local = __builtin_amdgcn_readfirstlane(found[1]);
+        slot = __builtin_amdgcn_readfirstlane(found[2]);
+        most = __builtin_amdgcn_readfirstlane(found[3]);
+        out->tok0 = __builtin_amdgcn_readfirstlane(found[4]);
+        n = __builtin_amdgcn_readfirstlane(found[5]);
+        seq = __builtin_amdgcn_readfirstlane(found[6]);
     }
-    __syncthreads();
-    out->b = __builtin_amdgcn_readfirstlane(found[0]);
-    if (out->b < 0) return false;
-    const int local = __builtin_amdgcn_readfirstlane(found[1]), most = __builtin_amdgcn_readfirstlane(found[3]);
-    const int tiles = (__builtin_amdgcn_readfirstlane(found[5]) * p.G + ROWS - 1) / ROWS, nth = local / most;
+    const int tiles = (n * p.G + ROWS - 1) / ROWS, nth = local / most;
     const int tile = tiles - 1 - nth;                        // the last rows see most keys: they come first
-    out->tok0 = __builtin_amdgcn_readfirstlane(found[4]);
-    out->n = __builtin_amdgcn_readfirstlane(found[5]);
-    out->ctx = __builtin_amdgcn_readfirstlane(found[6]) - out->n;
+    out->n = n;
+    out->ctx = seq - n;
     out->row0 = tile * ROWS;
     out->rows = min(ROWS, out->n * p.G - out->row0);
-    const int first = out->ctx + out->row0 / p.G, last = out->ctx + (out->row0 + out->rows - 1) / p.G;
+    const int first = out->ctx + token_of(p, out->row0), last = out->ctx + token_of(p, out->row0 + out->rows - 1);
     out->kv0 = p.window ? max(0, first - p.window + 1) : 0;
     out->kv1 = last + 1;                                     // (not above the length; 0 and less where nothing is seen)
     // the tile's own blocks, which may be fewer than its request's: as many parts as they fill, of like size
     const int blocks = max(0, (out->kv1 + KEYS - 1) / KEYS - out->kv0 / KEYS);
     out->parts = min(most, parts_of(blocks));
     out->part = local - nth * most;
-    out->slot = __builtin_amdgcn_readfirstlane(found[2]) + nth * most;
+    out->slot = slot + nth * most;
     const int each = (blocks + out->parts - 1) / out->parts;
     out->k0 = out->kv0 / KEYS + out->part * each;
     out->k1 = min(out->k0 + each, out->kv0 / KEYS + blocks);
@@ -164,10 +190,11 @@ __device__ __forceinline__ float* partial_stats(const AttnParams& p, const AttnK
     return kind.partial + (int64_t)p.Hk * 2 * kind.pieces * rows * D + ((int64_t)head * 2 * kind.pieces + slot) * rows * 2;
 }
 
-// Rows of a padded batch get zeros: every workgroup a share, whatever it does else.
+// Rows of a padded batch, from `end` on, get zeros: every workgroup a share, whatever it does else.  (The end is read before the piece is found,
+// used after it: as a wait of its own it would be most of a microsecond.)
 template <int THREADS>
-__device__ __forceinline__ void clear_padding(const AttnParams& p, int D) {
-    const int64_t per_token = (int64_t)p.Hq * D / 8, first = min(max(p.start[p.B], 0), p.T) * per_token;
+__device__ __forceinline__ void clear_padding(const AttnParams& p, int end, int D) {
+    const int64_t per_token = (int64_t)p.Hq * D / 8, first = min(max(end, 0), p.T) * per_token;
     for (int64_t i = first + (int64_t)blockIdx.x * THREADS + threadIdx.x; i < p.T * per_token; i += (int64_t)gridDim.x * THREADS)
         reinterpret_cast<u32x4_t*>(p.out)[i] = (u32x4_t){0u, 0u, 0u, 0u};
 }
@@ -219,7 +246,7 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, const AttnKind& 
         }
         if (first == 0 && r < r1) {
             const float inv = l > 0.f ? 1.0f / l : 0.f;
-            const int row = w.row0 + r, tok = row / p.G;
+            const int row = w.row0 + r, tok = token_of(p, row);
             T4 y;
 #pragma unroll
             for (int j = 0; j < 4; ++j) y[j] = (T)(acc[j] * inv);
@@ -249,20 +276,23 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x8 T8;
     typedef typename Elem<TYPE>::x4 T4;
-    constexpr int KS = D / 32, DT = D / 16, STEP = 32, ROWS = 16 * NQ, KEYS = 4 * STEP;     // k-steps of K Q^T, 16-row tiles of O^T, keys of a step
+    constexpr int KS = D / 32, DT = D / 16, STEP = 32, ROWS = 16 * NQ, KEYS = kFewKeys;     // k-steps of K Q^T, 16-row tiles of O^T, keys of a step
     constexpr int SW_SHIFT = D == 64 ? 1 : 0, SW_MASK = D == 64 ? 3 : 7;
     constexpr int VI = STEP * D * 2 / 1024, CH = D / 8;      // loads of V, 16-byte pieces of a row
     __shared__ float stats[4][2][ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
     const int head = block % p.Hk;
+    const int end_of_tokens = p.start[p.B];
     Piece w;
-    if (!find_piece<ROWS, KEYS, false>(p, p.few.pieces, block / p.Hk, &w)) return;
+    const bool found = find_piece<ROWS, KEYS, false>(p, p.few.pieces, block / p.Hk, &w);
+    clear_padding<256>(p, end_of_tokens, D);
+    if (!found) return;
 
     T8 q[NQ][KS];
     int pos[NQ];                                             // (negative where the length is below the number of new tokens)
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
-        const int row = w.row0 + min(16 * n + col, w.rows - 1), tok = row / p.G, qh = head * p.G + row - tok * p.G;
+        const int row = w.row0 + min(16 * n + col, w.rows - 1), tok = token_of(p, row), qh = head * p.G + row - tok * p.G;
         pos[n] = w.ctx + tok;
         const T* const qp = static_cast<const T*>(p.q) + (int64_t)(w.tok0 + tok) * p.q_stride + (int64_t)qh * D + grp * 8;
 #pragma unroll
@@ -282,7 +312,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
     const int ps = 1 << p.shift;
     // keys that every row sees need no masks
     const int window = p.window ? p.window : 0x7FFFFFFF;     // (a position less this does not wrap: lengths are up to 2^30)
-    const int all0 = p.window ? w.ctx + (w.row0 + w.rows - 1) / p.G - p.window + 1 : 0, all1 = w.ctx + w.row0 / p.G + 1;
+    const int all0 = p.window ? w.ctx + token_of(p, w.row0 + w.rows - 1) - p.window + 1 : 0, all1 = w.ctx + token_of(p, w.row0) + 1;
     const int end = min(w.kv1, w.k1 * KEYS);
     int ids = 0;                                             // lane i: the page of the 16 keys that are number i of 64 this wavefront comes to
 
@@ -432,7 +462,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
                 }
             } else {
                 const float inv = den > 0.f ? 1.0f / den : 0.f;
-                const int row = w.row0 + 16 * n + r, tok = row / p.G;
+                const int row = w.row0 + 16 * n + r, tok = token_of(p, row);
                 T4 y;
 #pragma unroll
                 for (int j = 0; j < 4; ++j) y[j] = (T)(acc[j] * inv);
@@ -471,10 +501,13 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
     static_assert(LOADS >= 1 && MINE <= 16, "a wavefront's share of a block is in one page");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
     const int head = block_no % p.Hk;
+    const int end_of_tokens = p.start[p.B];
     Piece w;
-    if (!find_piece<kTileRows, KEYS, false>(p, p.many.pieces, block_no / p.Hk, &w)) return;
+    const bool found = find_piece<kTileRows, KEYS, false>(p, p.many.pieces, block_no / p.Hk, &w);
+    clear_padding<256>(p, end_of_tokens, D);
+    if (!found) return;
 
-    const int wrow = wave * 32, row = w.row0 + min(wrow + col, w.rows - 1), tok = row / p.G, qh = head * p.G + row - tok * p.G;
+    const int wrow = wave * 32, row = w.row0 + min(wrow + col, w.rows - 1), tok = token_of(p, row), qh = head * p.G + row - tok * p.G;
     const int pos = w.ctx + tok;
     T8 q[KS];
     {
@@ -492,7 +525,7 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
     const int ps = 1 << p.shift;
     // keys that every row of this wavefront sees need no masks; those that none sees no work
     const int lo_row = w.row0 + min(wrow, w.rows - 1), hi_row = w.row0 + min(wrow + 31, w.rows - 1);
-    const int pos_lo = w.ctx + __builtin_amdgcn_readfirstlane(lo_row / p.G), pos_hi = w.ctx + __builtin_amdgcn_readfirstlane(hi_row / p.G);
+    const int pos_lo = w.ctx + __builtin_amdgcn_readfirstlane(token_of(p, lo_row)), pos_hi = w.ctx + __builtin_amdgcn_readfirstlane(token_of(p, hi_row));
     const int window = p.window ? p.window : 0x7FFFFFFF;
     const int all0 = p.window ? pos_hi - p.window + 1 : 0, all1 = pos_lo + 1;
     const int any0 = p.window ? pos_lo - p.window + 1 : 0, any1 = wrow < w.rows ? pos_hi + 1 : 0;
@@ -679,7 +712,6 @@ template <int TYPE, int D, int NQ>
 __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) void attend_few_kernel(const AttnParams p) {
     __shared__ __align__(16) uint8_t lds[4][few_lds_bytes(D)];
     uint8_t* const buf[4] = {lds[0], lds[1], lds[2], lds[3]};
-    clear_padding<256>(p, D);
     attend_few<TYPE, D, NQ>(p, blockIdx.x, buf);
 }
 
@@ -688,7 +720,6 @@ template <int TYPE, int D>
 __global__ __launch_bounds__(256, 2) void attend_mixed_kernel(const AttnParams p) {
     constexpr int STAGE = tile_keys(D) * D * 2, BYTES = STAGE > few_lds_bytes(D) ? STAGE : few_lds_bytes(D);
     __shared__ __align__(16) uint8_t lds_k0[BYTES], lds_k1[BYTES], lds_v0[BYTES], lds_v1[BYTES];
-    clear_padding<256>(p, D);
     const int tiles = p.many.most * p.Hk;
     if ((int)blockIdx.x < tiles) {
         attend_many<TYPE, D>(p, blockIdx.x, lds_k0, lds_k1, lds_v0, lds_v1);
@@ -700,14 +731,14 @@ __global__ __launch_bounds__(256, 2) void attend_mixed_kernel(const AttnParams p
 
 template <int TYPE, int D, int ROWS>
 __global__ __launch_bounds__(256) void join_few_kernel(const AttnParams p) {
-    join_parts<TYPE, D, ROWS, 128>(p, p.few, blockIdx.x);
+    join_parts<TYPE, D, ROWS, kFewKeys>(p, p.few, blockIdx.x);
 }
 
 template <int TYPE, int D>
 __global__ __launch_bounds__(256) void join_mixed_kernel(const AttnParams p) {
-    const int tiles = 2 * p.many.pieces * p.Hk;
+    const int tiles = p.many.slots * p.Hk;
     if ((int)blockIdx.x < tiles) join_parts<TYPE, D, kTileRows, tile_keys(D)>(p, p.many, blockIdx.x);
-    else join_parts<TYPE, D, 16, 128>(p, p.few, blockIdx.x - tiles);
+    else join_parts<TYPE, D, 16, kFewKeys>(p, p.few, blockIdx.x - tiles);
 }
 
 // The launch for a call: whether requests may have more than kFew rows, the rows of a tile of few (16 or 32), and the pieces aimed at over all KV heads.
@@ -738,26 +769,26 @@ template <int TYPE, int D>
 static void launch_attention(const AttnParams& p, const AttnPlan& a, hipStream_t st) {
     if (a.mixed) {
         hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D>), dim3((unsigned)((p.many.most + p.few.most) * p.Hk)), dim3(256), 0, st, p);
-        const unsigned slots = 2 * (p.many.pieces + p.few.pieces) * p.Hk;
+        const unsigned slots = (p.many.slots + p.few.slots) * p.Hk;
         if (slots) hipLaunchKernelGGL((join_mixed_kernel<TYPE, D>), dim3(slots), dim3(256), 0, st, p);
         return;
     }
-    const dim3 grid((unsigned)(p.few.most * p.Hk)), join((unsigned)(2 * p.few.pieces * p.Hk));
+    const dim3 grid((unsigned)(p.few.most * p.Hk)), join((unsigned)(p.few.slots * p.Hk));
     if constexpr (D < 256) {
         if (a.rows == 32) {
             hipLaunchKernelGGL((attend_few_kernel<TYPE, D, 2>), grid, dim3(256), 0, st, p);
-            if (p.few.pieces) hipLaunchKernelGGL((join_few_kernel<TYPE, D, 32>), join, dim3(256), 0, st, p);
+            if (p.few.slots) hipLaunchKernelGGL((join_few_kernel<TYPE, D, 32>), join, dim3(256), 0, st, p);
             return;
         }
     }
     hipLaunchKernelGGL((attend_few_kernel<TYPE, D, 1>), grid, dim3(256), 0, st, p);
-    if (p.few.pieces) hipLaunchKernelGGL((join_few_kernel<TYPE, D, 16>), join, dim3(256), 0, st, p);
+    if (p.few.slots) hipLaunchKernelGGL((join_few_kernel<TYPE, D, 16>), join, dim3(256), 0, st, p);
 }
 
 }  // namespace rtn
 
 extern "C" size_t rtn_paged_attention_workspace_nbytes(int64_t tokens, int n_requests, int q_heads, const rtn_kv_cache* cache, int max_new) {
-    if (rtn::check_cache(cache) != RTN_OK || tokens < 0 || tokens > 1 << 24 || n_requests < 1 || n_requests > 65536 || q_heads < 1 ||
+    if (rtn::check_cache(cache) != RTN_OK || tokens < 0 || tokens > 1 << 20 || n_requests < 1 || n_requests > 65536 || q_heads < 1 ||
         q_heads % cache->kv_heads != 0 || q_heads / cache->kv_heads > 64 || max_new < 1)
         return 0;
     return rtn::plan_attention(tokens, n_requests, q_heads, cache->kv_heads, cache->head_dim, max_new).bytes(cache->kv_heads, cache->head_dim);
@@ -771,7 +802,7 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     if (st != RTN_OK) return st;
     if (!dev_block_table || !dev_seq_lens || !dev_query_start || (tokens != 0 && (!dev_q || !dev_out))) return RTN_ERR_NULL;
     const int D = cache->head_dim;
-    if (tokens < 0 || tokens > 1 << 24 || n_requests < 1 || n_requests > 65536 || q_heads < 1 || q_heads % cache->kv_heads != 0 ||
+    if (tokens < 0 || tokens > 1 << 20 || n_requests < 1 || n_requests > 65536 || q_heads < 1 || q_heads % cache->kv_heads != 0 ||
         q_heads / cache->kv_heads > 64 || q_stride < (int64_t)q_heads * D || q_stride > (int64_t)1 << 36 || max_blocks < 1 ||
         max_blocks > (1 << 30) / cache->page_size || table_stride < max_blocks || max_new < 1)
         return RTN_ERR_SHAPE;
@@ -793,12 +824,20 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     const int64_t few_tiles = std::min(rows / a.rows + n_requests, a.mixed ? (int64_t)n_requests * (rtn::kFew / a.rows) : rows);
     const int64_t many_tiles = a.mixed ? rows / rtn::kTileRows + std::min<int64_t>(n_requests, rows / rtn::kFew) : 0;
     if ((few_tiles + a.few + many_tiles + a.many) * Hk >= 0x7FFFFFFF) return RTN_ERR_SHAPE;
+    auto bounds = [&](int64_t tiles, int pieces, int keys, int* most, int* slots) {
+        const int64_t parts = ((int64_t)max_blocks * cache->page_size + keys - 1) / keys;     // of the longest request that the table holds
+        *most = (int)std::min(tiles + pieces, tiles * parts);
+        *slots = (int)std::min((int64_t)2 * pieces, tiles * parts);
+    };
+    int few_most, few_slots, many_most, many_slots;
+    bounds(few_tiles, a.few, rtn::kFewKeys, &few_most, &few_slots);
+    bounds(many_tiles, a.many, rtn::tile_keys(D), &many_most, &many_slots);
     const float log2e = 1.4426950408889634f;
     float* const ws = static_cast<float*>(dev_workspace);
     const rtn::AttnParams p = {dev_q, cache->dev_k, cache->dev_v, dev_out, dev_block_table, dev_seq_lens, dev_query_start, q_stride, cache->page_stride,
                                cache->head_stride, cache->token_stride, table_stride, (int)cache->pages, rtn::log2_of(cache->page_size), max_blocks,
                                n_requests, (int)tokens, q_heads, Hk, G, window, scale * log2e, softcap, softcap > 0.f ? scale / softcap : 0.f,
-                               softcap * log2e, a.mixed ? rtn::kFew : 0x7FFFFFFF, {ws + tiles_bytes / 4, a.few, (int)(few_tiles + a.few)}, {ws, a.many, (int)(many_tiles + a.many)}};
+                               softcap * log2e, G == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / G) + 1, G == 1 ? 0xFFFFFFFFu : 0u, a.mixed ? rtn::kFew : 0x7FFFFFFF, {ws + tiles_bytes / 4, a.few, few_most, few_slots}, {ws, a.many, many_most, many_slots}};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == RTN_TYPE_F16) {
         if (D == 64) rtn::launch_attention<RTN_TYPE_F16, 64>(p, a, s);
