@@ -409,6 +409,74 @@ def report_grouped(args, rtn, synth, torch, np, dev) -> int:
     return 0
 
 
+def report_attention(args, rtn, synth, torch, np, dev) -> int:
+    """A layer's attention block in token generation: rtn_cache_plan once a step, then the quantised QKV projection, rotation with the cache
+    write, attention over the pages and the quantised output projection, captured and replayed while the requests grow."""
+    shapes = {"8b": synth.LLAMA_8B, "70b": synth.LLAMA_70B, "405b": synth.LLAMA_405B}[args.report_attention]
+    bits, g, D, Hk, ps, cached = args.bits, 128 if args.bits == 4 else 0, 128, 8, 16, 4000
+    (K, N), (Ko, No) = shapes["qkv"], shapes["o"]
+    Hq = Ko // D
+    weights = []
+    for i, (n, k) in enumerate(((N, K), (No, Ko))):
+        weights.append(rtn.rtn_quantize(synth.normal_weight(n, k, 0.02, i, dev), bits, g))
+    angle = torch.arange(cached + 512, dtype=torch.float64)[:, None] * 500000.0 ** (-torch.arange(0, D, 2, dtype=torch.float64) / D)[None]
+    rope = torch.cat([angle.cos(), angle.sin()], 1).float().to(dev)
+    print(f"# {args.report_attention}, int{bits}, {Hq} query heads on {Hk} of {D}, requests of {cached} tokens and up, pages of {ps}; us per replay, one layer "
+          f"(caches of the replays in between are not cold: see the calls' own figures); cache TB/s over the attention's time")
+    for B in [int(x) for x in args.batches.split(",")]:
+        width = (cached + 512) // ps
+        pages = B * width
+        k, v = (torch.randn((pages, Hk, ps, D), device=dev, dtype=torch.float16) for _ in range(2))
+        cache = rtn.PagedCache(k, v)
+        table = torch.full((B, width), -1, dtype=torch.int32, device=dev)
+        free, count = torch.randperm(pages, device=dev).to(torch.int32), torch.tensor([pages], dtype=torch.int32, device=dev)
+        lens, step = torch.zeros(B, dtype=torch.int32, device=dev), torch.full((B,), cached, dtype=torch.int32, device=dev)
+        first = rtn.rtn_cache_plan(step, lens, table, free, count, ps, B * cached)           # the prompts' pages
+        lens.copy_(first.seq_lens), count.copy_(first.free_count)
+        assert int(first.status) == 0
+        step.fill_(1)
+        plan = rtn.CachePlan.empty(B, B, dev)._replace(seq_lens=lens, free_count=count)
+        x, qkv, out = synth.activation(B, K, 1, dev), torch.empty((B, N), dtype=torch.float16, device=dev), torch.empty((B, No), dtype=torch.float16, device=dev)
+        q, att = (torch.empty((B, Hq, D), dtype=torch.float16, device=dev) for _ in range(2))
+        ws = torch.empty(max(rtn.rtn_workspace_nbytes(B, N, K, bits, g), rtn.rtn_workspace_nbytes(B, No, Ko, bits, g),
+                             rtn.rtn_paged_attention_workspace_nbytes(B, B, Hq, cache, 1), 256), dtype=torch.uint8, device=dev)
+        calls = {
+            "plan": lambda: rtn.rtn_cache_plan(step, lens, table, free, count, ps, B, out=plan),
+            "qkv": lambda: rtn.rtn_linear(x, *weights[0], bits, g, out=qkv, workspace=ws),
+            "rope": lambda: rtn.rtn_rope_cache(qkv, Hq, rope, plan.positions, plan.slots, cache, out=q),
+            "attention": lambda: rtn.rtn_paged_attention(q, cache, table, plan.seq_lens, plan.query_start, 1, out=att, workspace=ws),
+            "o": lambda: rtn.rtn_linear(att.view(B, Hq * D), *weights[1], bits, g, out=out, workspace=ws),
+        }
+
+        def timed(names, times):
+            for n in names:
+                calls[n]()
+            torch.cuda.synchronize()
+            cg, st = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+            with torch.cuda.stream(st):
+                with torch.cuda.graph(cg, stream=st):
+                    for _ in range(times):
+                        for n in names:
+                            calls[n]()
+            ts = []
+            for _ in range(5):
+                e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+                e0.record()
+                cg.replay()
+                e1.record()
+                torch.cuda.synchronize()
+                ts.append(e0.elapsed_time(e1) * 1e3 / times)
+            return float(np.median(ts))
+
+        whole = timed(list(calls), 10)
+        parts = {n: timed([n], 20) for n in list(calls)[1:]}
+        assert int(plan.status) == 0 and torch.isfinite(out).all()
+        nbytes = int(lens.sum()) * Hk * D * 4
+        print(f"B={B:3d}  block {whole:8.1f} us  " + "  ".join(f"{n} {t:7.1f}" for n, t in parts.items()) + f"  cache {nbytes / parts['attention'] / 1e6:5.2f} TB/s", flush=True)
+        del cache, k, v
+    return 0
+
+
 def main() -> int:
     ap = argparse.ArgumentParser()
     ap.add_argument("--gpus", type=int, default=1)
@@ -430,6 +498,8 @@ def main() -> int:
                     help="instead of the JSON line, time a plain read kernel on buffers of every workload matrix's packed size and on 512 MB")
     ap.add_argument("--report-grouped", action="store_true",
                     help="instead of the JSON line, time expert-like independent modules serially and through the grouped call")
+    ap.add_argument("--report-attention", choices=["8b", "70b", "405b"], default=None,
+                    help="a layer's attention block in token generation over a paged KV cache: projections, rotation, attention")
     ap.add_argument("--bits", type=int, default=4, help="--report only: 4 (group 128) or 8 (per-channel)")
     ap.add_argument("--selective", action="store_true",
                     help="--report only: the selective-precision layer (modules 2 and 4 at 8 bit per-channel, the others at 4 bit g128)")
@@ -459,6 +529,8 @@ def main() -> int:
         return report_crossover(args, rtn, synth, torch, np, dev)
     if args.report_load:
         return report_load(args, rtn, synth, torch, np, dev)
+    if args.report_attention:
+        return report_attention(args, rtn, synth, torch, np, dev)
     if args.report_grouped:
         return report_grouped(args, rtn, synth, torch, np, dev)
     if args.report_ceiling:

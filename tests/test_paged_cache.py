@@ -527,3 +527,149 @@ def test_attention_and_rope_run_on_the_current_stream_and_replay(rtn):
         assert lens.tolist() == [40, 40, 22, 40, 40]
     for a, b in zip(*results):
         assert torch.equal(a, b)
+
+
+# ---- many requests, large pools, streams, the binding's two ways -----------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("B", [64, 65, 200, 300, 1100])
+@pytest.mark.parametrize("chunks,window", [(0, 0), (3, 0), (3, 40)])
+def test_attention_of_many_requests(rtn, B, chunks, window):
+    """Up to 64 requests a wavefront finds its piece by itself, above a workgroup does, from 257 with several requests a thread."""
+    rng = np.random.default_rng(B + chunks)
+    lens = [(int(rng.integers(0, 90)), int(rng.integers(20, 60)) if i % (B // max(chunks, 1)) == 1 and chunks else int(rng.integers(0, 4))) for i in range(B)]
+    lens[B // 2] = (3000, 1)
+    _check_attention(rtn, torch.float16, lens, 4, 2, 64, 16, window=window, seed=B)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("Hq,Hk,new", [(64, 1, 1), (64, 1, 2), (7, 7, 70), (1, 1, 65), (30, 10, 3), (33, 1, 5)])
+def test_attention_of_head_layouts(rtn, Hq, Hk, new):
+    _check_attention(rtn, torch.bfloat16, [(300, new), (0, new), (77, max(1, new - 1))], Hq, Hk, 128, 32, seed=new)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", ["long", "mixed", "chunk"])
+def test_attention_with_every_size_of_workspace_is_right_and_repeats(rtn, lens):
+    """Less workspace: fewer pieces.  The same workspace: the same bits."""
+    args = _attention_case(torch.float16, LENGTHS[lens], 8, 2, 128, 16, seed=9)
+    q, k, v, table, seq, start = args
+    cache, new = rtn.PagedCache(k, v), max(n for _, n in LENGTHS[lens])
+    full = rtn.rtn_paged_attention_workspace_nbytes(q.shape[0], len(LENGTHS[lens]), 8, cache, new)
+    assert full > 0
+    want, mass, err = _attention_reference(q, k, v, table, LENGTHS[lens], 128 ** -0.5, 0.0, 0)
+    for nbytes in (0, 4096, full // 100 // 16 * 16, full // 7 // 16 * 16, full // 2 // 16 * 16, full):
+        outs = []
+        for _ in range(2):
+            ws = torch.full((max(nbytes, 1),), 0xFF, dtype=torch.uint8, device=DEV)[:nbytes]      # (NaN patterns: nothing in it is read before it is written)
+            outs.append(rtn.rtn_paged_attention(q, cache, table, seq, start, new, workspace=ws))
+        assert torch.equal(outs[0], outs[1])
+        assert ((outs[0].cpu().double() - want).abs() <= 2.0 ** -11 * (1.01 * want.abs() + 1.125 * mass) + err * mass + 6 * 2.0 ** -25 * 5000 ** -0.5 + 2.0 ** -24).all(), nbytes
+
+
+@pytest.mark.gpu
+def test_pools_beyond_32_bit_offsets(rtn):
+    """Pages whose elements lie beyond 2^32 bytes and 2^31 elements of a pool: rotation writes there, attention reads there."""
+    Hk, ps, D = 8, 16, 128
+    pages = (2 ** 32 // 2 + 2 ** 28) // (Hk * ps * D)                  # 2^31 + 2^28 elements, 4.8 GB a pool
+    k, v = (torch.zeros(pages, Hk, ps, D, dtype=torch.float16, device=DEV) for _ in range(2))
+    cache = rtn.PagedCache(k, v)
+    g = torch.Generator().manual_seed(3)
+    ids = torch.tensor([pages - 1, 5, pages - 7, pages // 2 + 1], dtype=torch.int32)
+    n, Hq = 60, 16
+    qkv = torch.randn(n, (Hq + 2 * Hk) * D, generator=g).half().to(DEV)
+    rope = torch.cat([torch.ones(64, D // 2), torch.zeros(64, D // 2)], 1).to(DEV)      # (no rotation)
+    pos = torch.arange(n, dtype=torch.int32)
+    slots = ids[pos.long() // ps] * ps + pos % ps
+    q = rtn.rtn_rope_cache(qkv, Hq, rope, pos.to(DEV), slots.to(torch.int32).to(DEV), cache)
+    heads = qkv.view(n, Hq + 2 * Hk, D)
+    assert torch.equal(q, heads[:, :Hq])
+    for pool, at in ((k, Hq), (v, Hq + Hk)):
+        assert torch.equal(pool[ids.long().to(DEV)].transpose(1, 2).reshape(-1, Hk, D)[:n], heads[:, at:at + Hk])
+    seq, start = torch.tensor([n], dtype=torch.int32, device=DEV), torch.tensor([0, n], dtype=torch.int32, device=DEV)
+    far = rtn.rtn_paged_attention(q, cache, ids[None].to(DEV), seq, start, n)
+    near = [torch.zeros(8, Hk, ps, D, dtype=torch.float16, device=DEV) for _ in range(2)]
+    for pool, small in ((k, near[0]), (v, near[1])):
+        small[:4] = pool[ids.long().to(DEV)]
+    assert torch.equal(far, rtn.rtn_paged_attention(q, rtn.PagedCache(*near), torch.arange(4, dtype=torch.int32, device=DEV)[None], seq, start, n))
+
+
+@pytest.mark.gpu
+def test_native_calls_are_the_python_calls(rtn, monkeypatch):
+    """The three calls by way of native code and by way of ctypes: the same launches, so the same bits; both on the stream that is current."""
+    from paper_2505_15909_amd import binding
+    if binding._native is None:
+        pytest.skip("the native part of the binding is not built")
+    q, k, v, table, seq, start = _attention_case(torch.bfloat16, LENGTHS["mixed"], 8, 2, 128, 16, layout="token")
+    qkv = torch.randn(50, 12 * 128, device=DEV).bfloat16()
+    rope = torch.randn(64, 96, device=DEV)
+    norm = torch.rand(128, device=DEV).bfloat16()
+    pos = torch.arange(50, dtype=torch.int32, device=DEV)
+    case = _plan_case(1, 90, 16, 30, 200, 50, 0.2, 3)
+    results, stream = [], torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for native in (True, False):
+        if not native:
+            monkeypatch.setattr(binding, "_native", None)
+        with torch.cuda.stream(stream):
+            kk, vv = k.clone(), v.clone()
+            cache = rtn.PagedCache(kk, vv)
+            ws = torch.empty(rtn.rtn_paged_attention_workspace_nbytes(q.shape[0], 5, 8, cache, 200), dtype=torch.uint8, device=DEV)
+            out = torch.empty_like(q)
+            rtn.rtn_paged_attention(q, cache, table, seq, start, 200, softcap=20.0, window=100, out=out, workspace=ws)
+            rot = rtn.rtn_rope_cache(qkv, 8, rope, pos, pos + 3, cache, norm, norm, eps=1e-5, interleaved=True, out=torch.empty(50, 8, 128, dtype=torch.bfloat16, device=DEV))
+            plan = _run_plan(case)
+        stream.synchronize()
+        results.append([out, rot, kk.nan_to_num(), vv.nan_to_num()] + [torch.as_tensor(x) for x in plan])
+    for a, b in zip(*results):
+        assert torch.equal(a, b)
+    # what is not plain goes to the Python code, and is refused there
+    with pytest.raises(ValueError):
+        rtn.rtn_paged_attention(q.float(), rtn.PagedCache(k, v), table, seq, start, 200, out=torch.empty_like(q), workspace=results[0][0])
+    with pytest.raises(ValueError):
+        rtn.rtn_rope_cache(qkv, 8, rope.half(), pos, pos, rtn.PagedCache(k, v), out=results[0][1])
+    with pytest.raises(rtn.RtnError):
+        rtn.rtn_rope_cache(qkv, 8, rope[:, :60].contiguous(), pos, pos, rtn.PagedCache(k, v), out=results[0][1])
+
+
+@pytest.mark.gpu
+def test_attention_block_with_quantised_projections(rtn):
+    """The calls as a layer makes them: quantised QKV projection, rotation with the cache write, attention, quantised output projection, over two
+    steps (a prompt, then a token), against the same in float64 on the dequantised weights."""
+    from paper_2505_15909_amd import synth
+    B, Hq, Hk, D, ps, hidden, bits, g = 3, 8, 2, 64, 16, 512, 4, 128
+    Wqkv, Wo = synth.normal_weight((Hq + 2 * Hk) * D, hidden, 0.05, 1, DEV), synth.normal_weight(hidden, Hq * D, 0.05, 2, DEV)
+    packed = [rtn.rtn_quantize(w, bits, g) for w in (Wqkv, Wo)]
+    dense = [rtn.rtn_dequantize(*w, K, bits, g).cpu().double() for w, K in zip(packed, (hidden, Hq * D))]
+    angle = torch.arange(64)[:, None] * 10000.0 ** (-torch.arange(0, D, 2) / D)[None]
+    rope = torch.cat([angle.cos(), angle.sin()], 1).float().to(DEV)
+    k, v = (torch.zeros(16, Hk, ps, D, dtype=torch.float16, device=DEV) for _ in range(2))
+    cache = rtn.PagedCache(k, v)
+    table = torch.full((B, 4), -1, dtype=torch.int32, device=DEV)
+    free, count = torch.randperm(16, device=DEV).to(torch.int32), torch.tensor([16], dtype=torch.int32, device=DEV)
+    lens, K64, V64 = torch.zeros(B, dtype=torch.int32, device=DEV), [None] * B, [None] * B
+    for seed, new in ((3, [17, 5, 30]), (4, [1, 1, 1])):
+        T = sum(new)
+        x = synth.activation(T, hidden, seed, DEV)
+        plan = rtn.rtn_cache_plan(torch.tensor(new, dtype=torch.int32, device=DEV), lens, table, free, count, ps, T)
+        qkv = rtn.rtn_linear(x, *packed[0], bits, g)
+        q = rtn.rtn_rope_cache(qkv, Hq, rope, plan.positions, plan.slots, cache)
+        att = rtn.rtn_paged_attention(q, cache, table, plan.seq_lens, plan.query_start, max(new))
+        out = rtn.rtn_linear(att.view(T, Hq * D), *packed[1], bits, g)
+        assert int(plan.status) == 0
+        lens, count = plan.seq_lens, plan.free_count
+        y = (x.cpu().double() @ dense[0].T).view(T, -1, D)
+        positions, at, ref = plan.positions.cpu(), 0, torch.zeros(T, Hq, D, dtype=torch.float64)
+        rot, _ = _rotated(y[:, :Hq + Hk], None, rope.cpu(), positions, D, False, 1e-6)
+        for b, n in enumerate(new):
+            s = slice(at, at + n)
+            K64[b] = rot[s, Hq:] if K64[b] is None else torch.cat([K64[b], rot[s, Hq:]])
+            V64[b] = y[s, Hq + Hk:] if V64[b] is None else torch.cat([V64[b], y[s, Hq + Hk:]])
+            for h in range(Hq):
+                sc = rot[s, h] @ K64[b][:, h // 4].T * D ** -0.5
+                sc = sc.masked_fill(torch.arange(len(K64[b]))[None] > positions[s][:, None], -np.inf)
+                ref[s, h] = torch.softmax(sc, -1) @ V64[b][:, h // 4]
+            at += n
+        ref = ref.reshape(T, -1) @ dense[1].T
+        # fp16 roundings of qkv, queries, keys, weights, attention and result: a few 2^-11 of the norms
+        assert (out.cpu().double() - ref).norm() <= 6 * 2.0 ** -11 * ref.norm()
