@@ -15,8 +15,7 @@
 namespace rtn {
 
 // Requests of up to kFew rows go to the workgroups for few rows, longer ones to those for many (kTileRows).
-constexpr int kFew = 64, kTileRows = 128;
-constexpr int kFewKeys = 128;                                // keys of a step of the four wavefronts of a workgroup for few rows
+constexpr int kFew = 64, kTileRows = 256;
 
 // One of the two kinds of workgroups in a launch.  `pieces` a KV head are aimed at (0: no request is split), and a head has room for twice as many
 // partial results, [Hk][2 pieces][rows][D] sums and, behind them, [Hk][2 pieces][rows][2] maxima and sums of weights.
@@ -59,13 +58,14 @@ struct Piece {
 // Each workgroup finds its own piece from the requests' lengths, which the host does not know: with n_b blocks of keys and t_b
 // tiles of rows, pieces of c = ceil(sum t_b n_b / `pieces`) blocks put a like share of the whole batch's keys on every workgroup, whatever the
 // requests' lengths; tile t of request b has the t_b ceil(n_b / c) pieces after those of the requests before it.  Two scans over the requests, each
-// thread's (one, up to 256 of them) read once.  `no` counts the pieces, or, JOIN, those of split requests alone.  All 256 threads call it.
-template <int ROWS, int KEYS, bool JOIN>
+// thread's own (one, up to as many requests as threads) read once.  `no` counts the pieces, or, JOIN, those of split requests alone.  All threads call it.
+template <int ROWS, int KEYS, bool JOIN, int WAVES>
 __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int no, Piece* out) {
-    __shared__ float totals[4];
-    __shared__ int sums[4][2], found[8];
+#pragma clang fp contract(off)                               // (the workgroups of a piece and those that join its parts come to the same shares)
+    __shared__ float totals[WAVES];
+    __shared__ int sums[WAVES][2], found[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int per = (p.B + 255) / 256, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
+    const int per = (p.B + 64 * WAVES - 1) / (64 * WAVES), b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     struct Request { int tok0, n, seq, tiles, blocks; };
     auto read = [&](int b) {
         Request r;
@@ -114,7 +114,10 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
         total = wave_scan(total);
         if (lane == 63) totals[wave] = total;
         __syncthreads();
-        c = shares((totals[0] + totals[1]) + (totals[2] + totals[3]));
+        total = 0.f;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) total += totals[w];
+        c = shares(total);
         int mine[2] = {0, 0};                                // pieces, and those of split requests
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
@@ -200,17 +203,17 @@ __device__ __forceinline__ void clear_padding(const AttnParams& p, int end, int 
 }
 
 // The parts of a tile's keys, brought to their common maximum and added up.  The workgroups of a tile, as many as it has parts, share its rows.
-// D / 4 threads take a row's sums of a part: 1024 / D rows at a time or, of fewer rows, several parts of them.
-template <int TYPE, int D, int ROWS, int KEYS>
+// D / 4 threads take a row's sums of a part: as many rows at a time as there are threads for or, of fewer rows, several parts of them.
+template <int TYPE, int D, int ROWS, int KEYS, int WAVES>
 __device__ __forceinline__ void join_parts(const AttnParams& p, const AttnKind& kind, int block) {
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x4 T4;
-    constexpr int LANES = D / 4, GROUPS = 256 / LANES;
+    constexpr int LANES = D / 4, GROUPS = 64 * WAVES / LANES;
     __shared__ __align__(16) float sums[GROUPS][D];
     __shared__ float stats[GROUPS][2];
     const int head = block % p.Hk, lane = threadIdx.x % LANES, group = threadIdx.x / LANES;
     Piece w;
-    if (!find_piece<ROWS, KEYS, true>(p, kind.pieces, block / p.Hk, &w) || w.parts == 1) return;
+    if (!find_piece<ROWS, KEYS, true, WAVES>(p, kind.pieces, block / p.Hk, &w) || w.parts == 1) return;
     const float *const po = partial_sums(p, kind, head, w.slot, ROWS, D) + lane * 4, *const pm = partial_stats(p, kind, head, w.slot, ROWS, D);
     const int r0 = w.rows * w.part / w.parts, r1 = w.rows * (w.part + 1) / w.parts;
     int at_once = 1;                                         // rows; the other groups share a row's parts
@@ -266,26 +269,27 @@ __device__ __forceinline__ void wave_sync() {
 template <int D>
 __device__ __forceinline__ int k_swizzle(int row) { return D == 64 ? (row >> 1) & 7 : row & 15; }
 
-// Few rows: 16 NQ of them a workgroup, whose four wavefronts take blocks of 32 keys in turn, each with a softmax of its own until they join
+// Few rows: 16 NQ of them a workgroup, whose wavefronts take blocks of 32 keys in turn, each with a softmax of its own until they join
 // at the end.  Bound by the reading of K and V, which go through LDS one after the other, 8 KiB that only its wavefront touches (D = 128), so that
 // the loop has no barrier.
+constexpr int few_keys(int waves) { return 32 * waves; }              // of a step of the wavefronts
 constexpr int few_lds_bytes(int D) { return 16 * (D + 4) * 4; }        // of a wavefront: 32 rows of V, and, later, sums of 16 rows
 
-template <int TYPE, int D, int NQ>
-__device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8_t* const (&buf)[4]) {
+template <int TYPE, int D, int NQ, int WAVES>
+__device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8_t* const (&buf)[WAVES], uint8_t* const vb) {
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x8 T8;
     typedef typename Elem<TYPE>::x4 T4;
-    constexpr int KS = D / 32, DT = D / 16, STEP = 32, ROWS = 16 * NQ, KEYS = kFewKeys;     // k-steps of K Q^T, 16-row tiles of O^T, keys of a step
+    constexpr int KS = D / 32, DT = D / 16, STEP = 32, ROWS = 16 * NQ, KEYS = few_keys(WAVES);     // k-steps of K Q^T, 16-row tiles of O^T, keys of a step
     constexpr int SW_SHIFT = D == 64 ? 1 : 0, SW_MASK = D == 64 ? 3 : 7;
     constexpr int VI = STEP * D * 2 / 1024, CH = D / 8;      // loads of V, 16-byte pieces of a row
-    __shared__ float stats[4][2][ROWS];
+    __shared__ float stats[WAVES][2][ROWS];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, grp = lane >> 4;
     const int head = block % p.Hk;
     const int end_of_tokens = p.start[p.B];
     Piece w;
-    const bool found = find_piece<ROWS, KEYS, false>(p, p.few.pieces, block / p.Hk, &w);
-    clear_padding<256>(p, end_of_tokens, D);
+    const bool found = find_piece<ROWS, KEYS, false, WAVES>(p, p.few.pieces, block / p.Hk, &w);
+    clear_padding<64 * WAVES>(p, end_of_tokens, D);
     if (!found) return;
 
     T8 q[NQ][KS];
@@ -307,7 +311,6 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
 #pragma unroll
         for (int t = 0; t < DT; ++t) o[n][t] = (float4_t){0.f, 0.f, 0.f, 0.f};
     }
-    uint8_t* const vb = wave == 0 ? buf[0] : wave == 1 ? buf[1] : wave == 2 ? buf[2] : buf[3];
     const int32_t* const table = p.table + (int64_t)w.b * p.table_stride;
     const int ps = 1 << p.shift;
     // keys that every row sees need no masks
@@ -420,7 +423,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
         }
         wave_sync();
     }
-    // the four wavefronts' keys, 16 rows at a time
+    // the wavefronts' keys, 16 rows at a time
 #pragma unroll
     for (int n = 0; n < NQ; ++n) {
         l[n] += __shfl_xor(l[n], 16);
@@ -437,16 +440,16 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
 #pragma unroll
         for (int t = 0; t < DT; ++t) *reinterpret_cast<float4_t*>(mine + t * 16 + grp * 4) = o[n][t];
         __syncthreads();
-        for (int i = tid; i < min(16, w.rows - 16 * n) * (D / 4); i += 256) {
+        for (int i = tid; i < min(16, w.rows - 16 * n) * (D / 4); i += 64 * WAVES) {
             const int r = i / (D / 4), d = i % (D / 4) * 4;
             float top = -INFINITY;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) top = fmaxf(top, stats[x][0][16 * n + r]);
+            for (int x = 0; x < WAVES; ++x) top = fmaxf(top, stats[x][0][16 * n + r]);
             const float base = top == -INFINITY ? 0.f : top;
             float4_t acc = {0.f, 0.f, 0.f, 0.f};
             float den = 0.f;
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
+            for (int x = 0; x < WAVES; ++x) {
                 const float f = exp2_of(stats[x][0][16 * n + r] - base);
                 den += f * stats[x][1][16 * n + r];
                 const float4_t y = *reinterpret_cast<const float4_t*>(reinterpret_cast<const float*>(buf[x]) + r * (D + 4) + d);
@@ -481,9 +484,12 @@ __device__ __forceinline__ void landed() {
     asm volatile("" ::: "memory");
 }
 
-// Many rows: 128 of them a workgroup, 32 a wavefront, over blocks of KEYS keys that are staged in LDS, the next block on its way while one is
-// worked on.  Bound by the matrix cores and, about as much, by the exponentials: two workgroups share a compute unit, so that one's
-// products run beside the other's softmax.  Rows of a staged block are permuted by 16-byte pieces (K: by the key's last four
+// Many rows: 256 of them a workgroup, 32 a wavefront, over blocks of KEYS keys that are staged in LDS, the next block on its way while one is
+// worked on.  Bound by the matrix cores and, about as much, by the exponentials, at a clock that the power lets go down to 1.6 GHz: what counts is
+// what is moved for a product.  Of a compute unit's eight wavefronts, two to a SIMD, one's products run beside the other's softmax.  (Two workgroups of 128 rows,
+// which bring each block twice: 2000 tokens over 30001 2002 us, 1881 this way; 4096 tokens of a prompt 162 and 151.  A wavefront a SIMD with 64 rows, which
+// would read LDS half as often, keeps its sums where the softmax cannot use them and takes 2.9 ms; halves of the keys half a step apart, two barriers a
+// block, 2.1.)  Rows of a staged block are permuted by 16-byte pieces (K: by the key's last four
 // bits; V: four pieces at a time by its last two, or, two rows of 64 lying side by side, the second of them), which spreads what the matrix operands read over all banks; the loads into LDS, whose
 // destinations are in lane order, take their sources permuted instead.
 __device__ __align__(16) uint32_t attention_zeros[4];        // what a key outside the request has for V
@@ -497,14 +503,14 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
     typedef typename Elem<TYPE>::x4 T4;
     constexpr int KEYS = tile_keys(D), KS = D / 16, DT = D / 32, KT = KEYS / 32;  // k-steps of K Q^T, 32-row tiles of O^T, 32-key tiles of S^T
     constexpr int CH = D / 8, PER = 64 / CH;                 // 16-byte pieces of a row, rows a load of a wavefront brings
-    constexpr int MINE = KEYS / 4, LOADS = MINE / PER;       // rows of a block that a wavefront brings, in so many loads
+    constexpr int MINE = KEYS / 8, LOADS = MINE / PER;       // rows of a block that a wavefront brings, in so many loads
     static_assert(LOADS >= 1 && MINE <= 16, "a wavefront's share of a block is in one page");
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 31, hi = lane >> 5;
     const int head = block_no % p.Hk;
     const int end_of_tokens = p.start[p.B];
     Piece w;
-    const bool found = find_piece<kTileRows, KEYS, false>(p, p.many.pieces, block_no / p.Hk, &w);
-    clear_padding<256>(p, end_of_tokens, D);
+    const bool found = find_piece<kTileRows, KEYS, false, 8>(p, p.many.pieces, block_no / p.Hk, &w);
+    clear_padding<512>(p, end_of_tokens, D);
     if (!found) return;
 
     const int wrow = wave * 32, row = w.row0 + min(wrow + col, w.rows - 1), tok = token_of(p, row), qh = head * p.G + row - tok * p.G;
@@ -712,41 +718,44 @@ template <int TYPE, int D, int NQ>
 __global__ __launch_bounds__(256, D == 64 ? 4 : D == 128 && NQ == 1 ? 3 : 2) void attend_few_kernel(const AttnParams p) {
     __shared__ __align__(16) uint8_t lds[4][few_lds_bytes(D)];
     uint8_t* const buf[4] = {lds[0], lds[1], lds[2], lds[3]};
-    attend_few<TYPE, D, NQ>(p, blockIdx.x, buf);
+    attend_few<TYPE, D, NQ, 4>(p, blockIdx.x, buf, lds[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]);
 }
 
 // Requests of few rows and of many in one launch: the tiles' products run beside the others' reading.
 template <int TYPE, int D>
-__global__ __launch_bounds__(256, 2) void attend_mixed_kernel(const AttnParams p) {
-    constexpr int STAGE = tile_keys(D) * D * 2, BYTES = STAGE > few_lds_bytes(D) ? STAGE : few_lds_bytes(D);
+__global__ __launch_bounds__(512, 2) void attend_mixed_kernel(const AttnParams p) {
+    constexpr int STAGE = tile_keys(D) * D * 2, FEW = few_lds_bytes(D), BYTES = STAGE > 2 * FEW ? STAGE : 2 * FEW;
     __shared__ __align__(16) uint8_t lds_k0[BYTES], lds_k1[BYTES], lds_v0[BYTES], lds_v1[BYTES];
     const int tiles = p.many.most * p.Hk;
     if ((int)blockIdx.x < tiles) {
         attend_many<TYPE, D>(p, blockIdx.x, lds_k0, lds_k1, lds_v0, lds_v1);
     } else {
-        uint8_t* const buf[4] = {lds_k0, lds_k1, lds_v0, lds_v1};
-        attend_few<TYPE, D, 1>(p, blockIdx.x - tiles, buf);
+        uint8_t* const buf[8] = {lds_k0, lds_k0 + FEW, lds_k1, lds_k1 + FEW, lds_v0, lds_v0 + FEW, lds_v1, lds_v1 + FEW};
+        const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        uint8_t* const mine = (wave < 4 ? wave < 2 ? lds_k0 : lds_k1 : wave < 6 ? lds_v0 : lds_v1) + (wave & 1) * FEW;
+        attend_few<TYPE, D, 1, 8>(p, blockIdx.x - tiles, buf, mine);
     }
 }
 
 template <int TYPE, int D, int ROWS>
 __global__ __launch_bounds__(256) void join_few_kernel(const AttnParams p) {
-    join_parts<TYPE, D, ROWS, kFewKeys>(p, p.few, blockIdx.x);
+    join_parts<TYPE, D, ROWS, few_keys(4), 4>(p, p.few, blockIdx.x);
 }
 
 template <int TYPE, int D>
-__global__ __launch_bounds__(256) void join_mixed_kernel(const AttnParams p) {
+__global__ __launch_bounds__(512) void join_mixed_kernel(const AttnParams p) {
     const int tiles = p.many.slots * p.Hk;
-    if ((int)blockIdx.x < tiles) join_parts<TYPE, D, kTileRows, tile_keys(D)>(p, p.many, blockIdx.x);
-    else join_parts<TYPE, D, 16, kFewKeys>(p, p.few, blockIdx.x - tiles);
+    if ((int)blockIdx.x < tiles) join_parts<TYPE, D, kTileRows, tile_keys(D), 8>(p, p.many, blockIdx.x);
+    else join_parts<TYPE, D, 16, few_keys(8), 8>(p, p.few, blockIdx.x - tiles);
 }
 
 // The launch for a call: whether requests may have more than kFew rows, the rows of a tile of few (16 or 32), and the pieces aimed at over all KV heads.
 // Few rows, 768 workgroups at a time, bound by reading: 64 ragged requests of 64 heads with 768, 1024 and 2048 pieces 236, 228, 235 us, 8 of 32k on 128
-// heads 217, 204, 213, one of 4101 tokens 19.5, 19.8, 23.6.  Many rows, 512 at a time, bound by the matrix cores, where a last round of few workgroups
-// costs as much as a full one and parts more than whole tiles: three quarters of a round, since parts are rounded up (three pieces of
-// prompts on 16 heads of 256 with 384, 512 and 1024 pieces 184, 247, 252 us).
-constexpr int kPieces = 1024, kTilePieces = 384;
+// heads 217, 204, 213, one of 4101 tokens 19.5, 19.8, 23.6 (the kernel of the time).  Beside tiles, in workgroups twice as large, half as many.  Many rows,
+// 256 at a time, bound by the matrix cores, where a last round of few workgroups costs as much as a full one and parts more than whole
+// tiles: three quarters of a round, since parts are rounded up (three pieces of prompts on 16 heads of 256 with 128, 192 and 256 pieces
+// 211, 146, 189 us; 1024 tokens over 8000 on 32 heads of 256 616, 396, 397).
+constexpr int kPieces = 1024, kMixedPieces = 512, kTilePieces = 192;
 
 struct AttnPlan {
     bool mixed;
@@ -760,7 +769,7 @@ static AttnPlan plan_attention(int64_t T, int B, int Hq, int Hk, int D, int max_
     AttnPlan a;
     a.mixed = rows > kFew;
     a.rows = a.mixed || rows <= 16 || D == 256 ? 16 : 32;
-    a.few = a.mixed && B == 1 ? 0 : (kPieces + Hk - 1) / Hk;
+    a.few = a.mixed && B == 1 ? 0 : ((a.mixed ? kMixedPieces : kPieces) + Hk - 1) / Hk;
     a.many = a.mixed ? (kTilePieces + Hk - 1) / Hk : 0;
     return a;
 }
@@ -768,9 +777,9 @@ static AttnPlan plan_attention(int64_t T, int B, int Hq, int Hk, int D, int max_
 template <int TYPE, int D>
 static void launch_attention(const AttnParams& p, const AttnPlan& a, hipStream_t st) {
     if (a.mixed) {
-        hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D>), dim3((unsigned)((p.many.most + p.few.most) * p.Hk)), dim3(256), 0, st, p);
+        hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D>), dim3((unsigned)((p.many.most + p.few.most) * p.Hk)), dim3(512), 0, st, p);
         const unsigned slots = (p.many.slots + p.few.slots) * p.Hk;
-        if (slots) hipLaunchKernelGGL((join_mixed_kernel<TYPE, D>), dim3(slots), dim3(256), 0, st, p);
+        if (slots) hipLaunchKernelGGL((join_mixed_kernel<TYPE, D>), dim3(slots), dim3(512), 0, st, p);
         return;
     }
     const dim3 grid((unsigned)(p.few.most * p.Hk)), join((unsigned)(p.few.slots * p.Hk));
@@ -830,7 +839,7 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
         *slots = (int)std::min((int64_t)2 * pieces, tiles * parts);
     };
     int few_most, few_slots, many_most, many_slots;
-    bounds(few_tiles, a.few, rtn::kFewKeys, &few_most, &few_slots);
+    bounds(few_tiles, a.few, rtn::few_keys(a.mixed ? 8 : 4), &few_most, &few_slots);
     bounds(many_tiles, a.many, rtn::tile_keys(D), &many_most, &many_slots);
     const float log2e = 1.4426950408889634f;
     float* const ws = static_cast<float*>(dev_workspace);
