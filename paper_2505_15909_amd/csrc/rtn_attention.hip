@@ -63,7 +63,7 @@ template <int ROWS, int KEYS, bool JOIN, int WAVES>
 __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int no, Piece* out) {
 #pragma clang fp contract(off)                               // (the workgroups of a piece and those that join its parts come to the same shares)
     __shared__ float totals[WAVES];
-    __shared__ int sums[WAVES][2], found[8];
+    __shared__ int counts[WAVES][2], sums[WAVES][2], found[8];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int per = (p.B + 64 * WAVES - 1) / (64 * WAVES), b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     struct Request { int tok0, n, seq, tiles, blocks; };
@@ -80,16 +80,20 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
         if (p.window) r.blocks = (int)min((int64_t)r.blocks, ((int64_t)p.window + ROWS / p.G + 1 + KEYS - 1) / KEYS + 1);
         return r;
     };
-    auto shares = [&](float total) {
+    // Blocks of a piece.  Few rows: where the tiles alone fill the compute units and the longest has little more than its share, none is split (64 requests of
+    // 1020 tokens 49 us split in two, 43 whole; of 300 to 8000 tokens 199 split, 210 with parts twice as long).
+    auto shares = [&](float total, int tiles, int longest) {
+        if (pieces == 0 || (ROWS <= kFew && 2 * tiles >= pieces && (float)longest * (float)tiles <= 1.25f * total)) return 1 << 30;
         // (not below the exact share, for the room that there is for partial results: the sums' rounding is less than 2^-10)
-        return pieces ? (int)fminf(0x1p30f, fmaxf(1.f, ceilf(total * (1.0f + 0x1p-10f) / (float)pieces))) : 1 << 30;
+        return (int)fminf(0x1p30f, fmaxf(1.f, ceilf(total * (1.0f + 0x1p-10f) / (float)pieces)));
     };
     int c, local, most, slot, n, seq;
     auto parts_of = [&](int blocks) { return max(1, (int)(((uint32_t)blocks + c - 1) / c)); };      // (up to 2^26 blocks)
     if (p.B <= 64) {                                         // a lane a request: each wavefront by itself, without LDS
         Request r = {};
         if (lane < p.B) r = read(lane);
-        c = shares(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan((float)r.tiles * (float)r.blocks)), 63)));
+        c = shares(__builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan((float)r.tiles * (float)r.blocks)), 63)),
+                   __builtin_amdgcn_readlane(wave_scan(r.tiles), 63), __builtin_amdgcn_readlane(wave_max(r.tiles ? r.blocks : 0), 63));
         const int parts = parts_of(r.blocks), have = r.tiles * parts, slots = parts > 1 ? have : 0;
         const int slots_before = wave_scan(slots) - slots, before = JOIN ? slots_before : wave_scan(have) - have;
         const uint64_t hit = __ballot(no >= before && no < before + (JOIN ? slots : have));
@@ -107,17 +111,31 @@ __device__ __forceinline__ bool find_piece(const AttnParams& p, int pieces, int 
         if (b0 < b1) own = read(b0);
         auto request = [&](int b) { return b == b0 ? own : read(b); };
         float total = 0.f;
+        int all = 0, longest = 0;
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
             total += (float)r.tiles * (float)r.blocks;
+            all += r.tiles;
+            longest = max(longest, r.tiles ? r.blocks : 0);
         }
         total = wave_scan(total);
-        if (lane == 63) totals[wave] = total;
+        all = wave_scan(all);
+        longest = wave_max(longest);
+        if (lane == 63) {
+            totals[wave] = total;
+            counts[wave][0] = all;
+            counts[wave][1] = longest;
+        }
         __syncthreads();
         total = 0.f;
+        all = longest = 0;
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) total += totals[w];
-        c = shares(total);
+        for (int w = 0; w < WAVES; ++w) {
+            total += totals[w];
+            all += counts[w][0];
+            longest = max(longest, counts[w][1]);
+        }
+        c = shares(total, all, longest);
         int mine[2] = {0, 0};                                // pieces, and those of split requests
         for (int b = b0; b < b1; ++b) {
             const Request r = request(b);
@@ -844,6 +862,9 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
         *most = (int)std::min(tiles + pieces, tiles * parts);
         *slots = (int)std::min((int64_t)2 * pieces, tiles * parts);
     };
+    // Requests of few rows of up to four steps of a workgroup are not split, and nothing is joined, where the table can hold no longer ones (one request of 250 tokens
+    // 8.9 us split, 6.5 whole, of 500 8.7 and 9.1; sixteen of 500 11.6 and 11.0).
+    if ((int64_t)max_blocks * cache->page_size <= 4 * 128) a.few = 0;
     int few_most, few_slots, many_most, many_slots;
     bounds(few_tiles, a.few, rtn::few_keys(a.mixed ? 8 : 4), &few_most, &few_slots);
     bounds(many_tiles, a.many, rtn::tile_keys(D), &many_most, &many_slots);

@@ -50,6 +50,17 @@ __device__ __forceinline__ T wave_scan(T x) {
     return x;
 }
 
+// The largest of the lanes up to this one, of values that are not negative.
+__device__ __forceinline__ int wave_max(int x) {
+    x = max(x, from_lane<0x111, 0xF>(x));
+    x = max(x, from_lane<0x112, 0xF>(x));
+    x = max(x, from_lane<0x114, 0xF>(x));
+    x = max(x, from_lane<0x118, 0xF>(x));
+    x = max(x, from_lane<0x142, 0xA>(x));
+    x = max(x, from_lane<0x143, 0xC>(x));
+    return x;
+}
+
 // Host-side checks.
 inline bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uintptr_t>(p) & (n - 1)) == 0; }
 
