@@ -318,7 +318,7 @@ enum { RTN_TYPE_F16 = 0, RTN_TYPE_BF16 = 1 };
 
 /* K and V pools of one layer: element (page, head, token of the page, d) is at page * page_stride + head * head_stride +
  * token * token_stride + d, in elements, in both.  page_size 16, 32, 64, 128 or 256; head_dim 64, 128 or 256; strides multiples of 8,
- * token_stride >= head_dim and page_size * token_stride <= 2^30; pages * page_size < 2^31; up to 1024 kv_heads.
+ * token_stride >= head_dim and page_size * token_stride <= 2^30; pages * page_size < 2^31; up to 1024 kv_heads; pools of up to 2^48 elements.
  * [pages][kv_heads][page_size][head_dim] keeps a head's page in one piece; [pages][page_size][kv_heads][head_dim] a token's heads. */
 typedef struct {
     void* dev_k;
@@ -364,7 +364,7 @@ rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev_cached_len
  *   dev_positions, dev_slots   in   int32 [tokens]; two tokens of a call must not have the same slot
  *   dev_q_norm, dev_k_norm     in   [head_dim] in the cache's type, or NULL: no norm
  *   dev_q_out      out  [tokens, q_heads, head_dim]
- * tokens 0 .. 2^24 (0: nothing to do). */
+ * tokens 0 .. 2^24 (0: nothing to do), tokens * (q_heads + 2 kv_heads) below 2^31. */
 rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_t qkv_stride, int q_heads, const float* dev_rope, int rotary_dim,
                           int64_t max_positions, int interleaved, const int32_t* dev_positions, const int32_t* dev_slots,
                           const void* dev_q_norm, const void* dev_k_norm, float eps, const rtn_kv_cache* cache, void* dev_q_out, void* stream);

@@ -237,7 +237,9 @@ __device__ __forceinline__ void join_parts(const AttnParams& p, const AttnKind& 
     int at_once = 1;                                         // rows; the other groups share a row's parts
     while (at_once < GROUPS && at_once < r1 - r0) at_once *= 2;
     const int by_parts = GROUPS / at_once, first = group & (by_parts - 1);
-    for (int r = r0 + group / by_parts; r < r1 + at_once - 1; r += at_once) {      // (as many turns for all groups)
+    const int turns = (r1 - r0 + at_once - 1) / at_once;     // as many for all groups: there are barriers in them
+    for (int turn = 0; turn < turns; ++turn) {
+        const int r = r0 + turn * at_once + group / by_parts;
         float4_t acc = {0.f, 0.f, 0.f, 0.f};
         float m = -INFINITY, l = 0.f;
         auto add = [&](float m2, float l2, const float4_t& x) {
@@ -332,7 +334,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
     const int32_t* const table = p.table + (int64_t)w.b * p.table_stride;
     const int ps = 1 << p.shift;
     // keys that every row sees need no masks
-    const int window = p.window ? p.window : 0x7FFFFFFF;     // (a position less this does not wrap: lengths are up to 2^30)
+    const int window = p.window ? p.window : 1 << 30;        // (no length is above 2^30)
     const int all0 = p.window ? w.ctx + token_of(p, w.row0 + w.rows - 1) - p.window + 1 : 0, all1 = w.ctx + token_of(p, w.row0) + 1;
     const int end = min(w.kv1, w.k1 * KEYS);
     int ids = 0;                                             // lane i: the page of the 16 keys that are number i of 64 this wavefront comes to
@@ -556,7 +558,7 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
     // keys that every row of this wavefront sees need no masks; those that none sees no work
     const int lo_row = w.row0 + min(wrow, w.rows - 1), hi_row = w.row0 + min(wrow + 31, w.rows - 1);
     const int pos_lo = w.ctx + __builtin_amdgcn_readfirstlane(token_of(p, lo_row)), pos_hi = w.ctx + __builtin_amdgcn_readfirstlane(token_of(p, hi_row));
-    const int window = p.window ? p.window : 0x7FFFFFFF;
+    const int window = p.window ? p.window : 1 << 30;
     const int all0 = p.window ? pos_hi - p.window + 1 : 0, all1 = pos_lo + 1;
     const int any0 = p.window ? pos_lo - p.window + 1 : 0, any1 = wrow < w.rows ? pos_hi + 1 : 0;
 
@@ -844,6 +846,7 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
         !rtn::aligned_to(dev_block_table, 4) || !rtn::aligned_to(dev_seq_lens, 4) || !rtn::aligned_to(dev_query_start, 4))
         return RTN_ERR_ALIGN;
     if (tokens == 0) return RTN_OK;
+    if (window >= 1 << 30) window = 0;                       // (as wide as any length)
     const int Hk = cache->kv_heads, G = q_heads / Hk;
     rtn::AttnPlan a = rtn::plan_attention(tokens, n_requests, q_heads, Hk, D, max_new);
     // a smaller workspace than asked for: fewer pieces of either kind

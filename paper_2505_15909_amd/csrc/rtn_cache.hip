@@ -195,11 +195,11 @@ __global__ __launch_bounds__(256) void rope_cache_kernel(const RopeParams p) {
     typedef typename Elem<TYPE>::x4 T4;
     constexpr int L = D / 8;                                 // lanes of a head
     const int H = p.Hq + 2 * p.Hk;
-    const int64_t row = (int64_t)blockIdx.x * (256 / L) + threadIdx.x / L;
+    const uint32_t row = blockIdx.x * (256 / L) + threadIdx.x / L;       // (below 2^31 + 32)
     const int c = threadIdx.x % L;
-    if (row >= (int64_t)p.tokens * H) return;                // (whole heads: the lanes of one stay together)
-    const int t = (int)(row / H), h = (int)(row - (int64_t)t * H);
-    const T* const src = static_cast<const T*>(p.qkv) + t * p.qkv_stride + h * D;
+    if (row >= (uint32_t)(p.tokens * H)) return;             // (whole heads: the lanes of one stay together)
+    const int t = (int)(row / (uint32_t)H), h = (int)(row - (uint32_t)t * H);
+    const T* const src = static_cast<const T*>(p.qkv) + t * p.qkv_stride + (int64_t)h * D;
     const bool rotated = h < p.Hq + p.Hk && c * 8 < p.rotary;
     const int e0 = INTERLEAVED || !rotated ? c * 8 : c * 4, e1 = INTERLEAVED || !rotated ? c * 8 + 4 : p.rotary / 2 + c * 4;
         const T4 x0 = *reinterpret_cast<const T4*>(src + e0), x1 = *reinterpret_cast<const T4*>(src + e1);
@@ -304,7 +304,7 @@ extern "C" rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_
         !rtn::aligned_to(dev_k_norm, 16) || !rtn::aligned_to(dev_q_out, 16) || !rtn::aligned_to(dev_positions, 4) || !rtn::aligned_to(dev_slots, 4))
         return RTN_ERR_ALIGN;
     if (!(eps >= 0.f) || (interleaved != 0 && interleaved != 1)) return RTN_ERR_CONFIG;
-    if (tokens * (q_heads + 2 * cache->kv_heads) / (2048 / D) >= 0x7FFFFFFF) return RTN_ERR_SHAPE;
+    if (tokens * (q_heads + 2 * cache->kv_heads) > 0x7FFFFFFF) return RTN_ERR_SHAPE;
     if (tokens == 0) return RTN_OK;
     const rtn::RopeParams p = {dev_qkv, dev_q_norm, dev_k_norm, dev_rope, dev_positions, dev_slots, dev_q_out, cache->dev_k, cache->dev_v, qkv_stride,
                                cache->page_stride, cache->head_stride, cache->token_stride, max_positions, cache->pages * cache->page_size, (int)tokens,

@@ -76,7 +76,8 @@ inline rtn_status check_cache(const rtn_kv_cache* c) {
     if (!page_size_valid(c->page_size) || c->kv_heads < 1 || c->kv_heads > 1024 || c->pages < 1 || c->pages > INT32_MAX / c->page_size) return RTN_ERR_SHAPE;
     if (c->page_stride < 0 || c->head_stride < 0 || c->token_stride < c->head_dim) return RTN_ERR_SHAPE;
     if (c->page_stride % 8 || c->head_stride % 8 || c->token_stride % 8) return RTN_ERR_ALIGN;
-    if (c->head_stride > (int64_t)1 << 40 || c->page_stride > (int64_t)1 << 40) return RTN_ERR_SHAPE;
+    // (offsets in bytes stay within 63 bits)
+    if ((double)c->page_stride * (double)c->pages + (double)c->head_stride * (double)c->kv_heads > 0x1p48) return RTN_ERR_SHAPE;
     if (c->token_stride > ((int64_t)1 << 30) / c->page_size) return RTN_ERR_SHAPE;
     if (!aligned_to(c->dev_k, 16) || !aligned_to(c->dev_v, 16)) return RTN_ERR_ALIGN;
     return RTN_OK;

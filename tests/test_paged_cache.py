@@ -84,6 +84,12 @@ def test_attention_refusals(kw, status):
     assert _attend(**kw) == status
 
 
+def test_sizes_beyond_the_offsets_are_refused():
+    assert _attend(cache=_cache(page_stride=1 << 40, pages=1 << 26)) == SHAPE
+    assert _rope(cache=_cache(head_stride=1 << 50)) == SHAPE
+    assert _rope(tokens=1 << 24, heads=128, stride=132 * 128) == SHAPE
+
+
 def test_binding_refuses_what_is_not_as_described():
     cpu = torch.zeros(4, 2, 16, 128, dtype=torch.float16)
     with pytest.raises(ValueError):
@@ -673,3 +679,24 @@ def test_attention_block_with_quantised_projections(rtn):
         ref = ref.reshape(T, -1) @ dense[1].T
         # fp16 roundings of qkv, queries, keys, weights, attention and result: a few 2^-11 of the norms
         assert (out.cpu().double() - ref).norm() <= 6 * 2.0 ** -11 * ref.norm()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", ["decode", "mixed"])
+def test_attention_in_windows_wider_than_any_length(rtn, lens):
+    """The widest window is no window, also where a length is below the number of new tokens."""
+    q, k, v, table, seq, start = _attention_case(torch.float16, LENGTHS[lens], 8, 2, 128, 16, seed=2)
+    cache, new = rtn.PagedCache(k, v), max(n for _, n in LENGTHS[lens])
+    seq = seq.clone()
+    seq[0] = max(1, int(seq[0]) - 3)
+    none = rtn.rtn_paged_attention(q, cache, table, seq, start, new)
+    for window in (2 ** 31 - 1, 2 ** 30, 2 ** 30 - 1):
+        assert torch.equal(rtn.rtn_paged_attention(q, cache, table, seq, start, new, window=window), none)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("Hq,Hk,lens", [(4, 2, [(700, 1)]), (6, 2, [(900, 1)]), (14, 2, [(600, 1), (2000, 1)]), (10, 2, [(5000, 2)]), (10, 2, [(3000, 11)]), (8, 1, [(4000, 9)])])
+def test_attention_joins_any_number_of_rows(rtn, D, Hq, Hk, lens):
+    """Rows and parts that do not divide one another: a tile's rows are shared by as many workgroups as it has parts."""
+    _check_attention(rtn, torch.float16, lens, Hq, Hk, D, 16, seed=Hq)
