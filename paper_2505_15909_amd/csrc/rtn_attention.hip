@@ -779,8 +779,8 @@ __global__ __launch_bounds__(512) void join_mixed_kernel(const AttnParams p) {
 // Few rows, 768 workgroups at a time, bound by reading: 64 ragged requests of 64 heads with 768, 1024 and 2048 pieces 236, 228, 235 us, 8 of 32k on 128
 // heads 217, 204, 213, one of 4101 tokens 19.5, 19.8, 23.6 (the kernel of the time).  Beside tiles, in workgroups twice as large, half as many.  Many rows,
 // 256 at a time, bound by the matrix cores, where a last round of few workgroups costs as much as a full one and parts more than whole
-// tiles: three quarters of a round, since parts are rounded up (three pieces of prompts on 16 heads of 256 with 128, 192 and 256 pieces
-// 211, 146, 189 us; 1024 tokens over 8000 on 32 heads of 256 616, 396, 397).
+// tiles: three quarters of a round, since parts are rounded up (three pieces of prompts on 16 heads of 256 with 160, 192, 224 and 256 pieces
+// 180, 145, 143, 190 us, beside 21 decode steps 210, 198, 201, 202; 1024 tokens over 8000 on 32 heads of 256 392 with each).
 constexpr int kPieces = 1024, kMixedPieces = 512, kTilePieces = 192;
 
 struct AttnPlan {
