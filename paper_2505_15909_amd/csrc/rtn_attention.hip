@@ -10,6 +10,7 @@
 #include "rtn_paged.h"
 
 #include <algorithm>
+#include <float.h>
 #include <math.h>
 
 namespace rtn {
@@ -30,7 +31,7 @@ struct AttnParams {
     const int32_t *table, *seq, *start;
     int64_t q_stride, page_stride, head_stride, token_stride, table_stride;
     int pages, shift, max_blocks, B, T, Hq, Hk, G, window;
-    float scale2, cap, cap_in, cap_out;                      // scale log2 e; softcap: cap_out tanh(cap_in q.k), cap_out = softcap log2 e
+    float scale2, cap, cap_in, cap_out;                      // scale log2 e; softcap: 2 scale log2 e / softcap, softcap log2 e
     uint32_t g_inv, g_one;                                   // row -> token is umulhi(row, g_inv) + (row & g_one): exact below 2^26 rows and G <= 64
     int few_rows;                                            // kFew, or no bound where the call's requests are all taken to have few
     AttnKind few, many;
@@ -41,10 +42,17 @@ __device__ __forceinline__ int token_of(const AttnParams& p, int row) { return (
 // exp2 of scores: the softmax is taken to base 2, with log2 e in the scale
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// cap_out tanh(x) = cap_out (1 - 2 / (e^2x + 1)); right at both ends, where e^2x is 0 or infinite
-__device__ __forceinline__ float capped(float x, float cap_out) {
-    const float e = exp2_of(x * 2.8853900817779268f);
-    return cap_out * (1.0f - 2.0f * __builtin_amdgcn_rcpf(e + 1.0f));
+// softcap tanh(x) log2 e, x = s scale / softcap, for s = q.k, with z = 2 x log2 e = cap_in s.  From |x| = 1/5 on cap_out (1 - 2 / (2^z + 1)), right at both ends, where
+// 2^z is 0 or infinite, with an error of a few ulps of the result.  Below, where that difference would leave an error of cap_out 2^-23 whatever the score, the
+// series of tanh(x) / x (its next term is below 2^-24) times the score without a cap: the error is relative to the score at any cap, one that makes z underflow
+// included.  (Both are formed first, so that the choice is no branch.)
+__device__ __forceinline__ float capped(const AttnParams& p, float s) {
+    constexpr double k = 0.12011325347955035;                // x^2 = k z^2
+    constexpr float c1 = (float)(-k / 3), c2 = (float)(2 * k * k / 15), c3 = (float)(-17 * k * k * k / 315), limit = 0.57707802f;
+    const float z = s * p.cap_in, y = z * z;
+    const float series = fmaf(y, fmaf(y, (y + c2 / c3) * c3, c1), 1.0f);         // (a sum and a product take their constants as they are, a register less)
+    const float small = s * p.scale2 * series, large = p.cap_out * (1.0f - 2.0f * __builtin_amdgcn_rcpf(exp2_of(z) + 1.0f));
+    return fabsf(z) < limit ? small : large;
 }
 
 // What a workgroup does: ROWS rows from row0 of request b, a part of their keys.
@@ -392,7 +400,7 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
         for (int n = 0; n < NQ; ++n) {
             float e[8], top = -INFINITY;
 #pragma unroll
-            for (int j = 0; j < 8; ++j) e[j] = p.cap > 0.f ? capped(s[n][j >> 2][j & 3] * p.cap_in, p.cap_out) : s[n][j >> 2][j & 3] * p.scale2;
+            for (int j = 0; j < 8; ++j) e[j] = p.cap > 0.f ? capped(p, s[n][j >> 2][j & 3]) : s[n][j >> 2][j & 3] * p.scale2;
             if (masked) {
 #pragma unroll
                 for (int j = 0; j < 8; ++j) {
@@ -522,7 +530,7 @@ __device__ __align__(16) uint32_t attention_zeros[4];        // what a key outsi
 
 constexpr int tile_keys(int D) { return D == 256 ? 32 : 64; }
 
-template <int TYPE, int D>
+template <int TYPE, int D, bool CAP>
 __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, uint8_t* lds_k0, uint8_t* lds_k1, uint8_t* lds_v0, uint8_t* lds_v1) {
     typedef typename Elem<TYPE>::one T;
     typedef typename Elem<TYPE>::x8 T8;
@@ -625,13 +633,12 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
         }
         __builtin_amdgcn_sched_barrier(0);
         __builtin_amdgcn_s_setprio(0);
-        float scale = p.scale2;
-        if (p.cap > 0.f) {
-            scale = 1.f;
+        const float scale = CAP ? 1.f : p.scale2;
+        if constexpr (CAP) {
 #pragma unroll
             for (int h = 0; h < KT; ++h)
 #pragma unroll
-                for (int j = 0; j < 16; ++j) s[h][j] = capped(s[h][j] * p.cap_in, p.cap_out);
+                for (int j = 0; j < 16; ++j) s[h][j] = capped(p, s[h][j]);
         }
         if (k0 < all0 || k0 + KEYS > all1) {
 #pragma unroll
@@ -747,14 +754,15 @@ __global__ __launch_bounds__(256, D == 64 && NQ == 1 ? 4 : D == 64 || (D == 128 
     attend_few<TYPE, D, NQ, 4>(p, blockIdx.x, buf, lds[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]);
 }
 
-// Requests of few rows and of many in one launch: the tiles' products run beside the others' reading.
-template <int TYPE, int D>
+// Requests of few rows and of many in one launch: the tiles' products run beside the others' reading.  Kernels apart for tiles with a cap and without (one for both
+// keeps the cap's registers where none is: 1024 tokens over 8000 on heads of 256 403 us, 392 so).
+template <int TYPE, int D, bool CAP>
 __global__ __launch_bounds__(512, 2) void attend_mixed_kernel(const AttnParams p) {
     constexpr int STAGE = tile_keys(D) * D * 2, FEW = few_lds_bytes(D), BYTES = STAGE > 2 * FEW ? STAGE : 2 * FEW;
     __shared__ __align__(16) uint8_t lds_k0[BYTES], lds_k1[BYTES], lds_v0[BYTES], lds_v1[BYTES];
     const int tiles = p.many.most * p.Hk;
     if ((int)blockIdx.x < tiles) {
-        attend_many<TYPE, D>(p, blockIdx.x, lds_k0, lds_k1, lds_v0, lds_v1);
+        attend_many<TYPE, D, CAP>(p, blockIdx.x, lds_k0, lds_k1, lds_v0, lds_v1);
     } else {
         uint8_t* const buf[8] = {lds_k0, lds_k0 + FEW, lds_k1, lds_k1 + FEW, lds_v0, lds_v0 + FEW, lds_v1, lds_v1 + FEW};
         const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -803,7 +811,9 @@ static AttnPlan plan_attention(int64_t T, int B, int Hq, int Hk, int D, int max_
 template <int TYPE, int D>
 static void launch_attention(const AttnParams& p, const AttnPlan& a, hipStream_t st) {
     if (a.mixed) {
-        hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D>), dim3((unsigned)((p.many.most + p.few.most) * p.Hk)), dim3(512), 0, st, p);
+        const dim3 grid((unsigned)((p.many.most + p.few.most) * p.Hk));
+        if (p.cap > 0.f) hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D, true>), grid, dim3(512), 0, st, p);
+        else hipLaunchKernelGGL((attend_mixed_kernel<TYPE, D, false>), grid, dim3(512), 0, st, p);
         const unsigned slots = (p.many.slots + p.few.slots) * p.Hk;
         if (slots) hipLaunchKernelGGL((join_mixed_kernel<TYPE, D>), dim3(slots), dim3(512), 0, st, p);
         return;
@@ -873,9 +883,11 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     bounds(many_tiles, a.many, rtn::tile_keys(D), &many_most, &many_slots);
     const float log2e = 1.4426950408889634f;
     float* const ws = static_cast<float*>(dev_workspace);
+    // (a cap so small that this passes fp32's range: scores of zero stay zero, all others are at the cap either way)
+    const float cap_in = softcap > 0.f ? (float)std::min(2.0 * scale / softcap * 1.4426950408889634, (double)FLT_MAX) : 0.f;
     const rtn::AttnParams p = {dev_q, cache->dev_k, cache->dev_v, dev_out, dev_block_table, dev_seq_lens, dev_query_start, q_stride, cache->page_stride,
                                cache->head_stride, cache->token_stride, table_stride, (int)cache->pages, rtn::log2_of(cache->page_size), max_blocks,
-                               n_requests, (int)tokens, q_heads, Hk, G, window, scale * log2e, softcap, softcap > 0.f ? scale / softcap : 0.f,
+                               n_requests, (int)tokens, q_heads, Hk, G, window, scale * log2e, softcap, cap_in,
                                softcap * log2e, G == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / G) + 1, G == 1 ? 0xFFFFFFFFu : 0u, a.mixed ? rtn::kFew : 0x7FFFFFFF, {ws + tiles_bytes / 4, a.few, few_most, few_slots}, {ws, a.many, many_most, many_slots}};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == RTN_TYPE_F16) {

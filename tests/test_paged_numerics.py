@@ -1,0 +1,64 @@
+"""The paged cache at the ends of its ranges: what test_paged_cache.py's sizes do not reach.  Against 64 bits, with bounds that do not grow with
+the parameter under test.
+
+u is the unit roundoff of the element type (2^-11 fp16, 2^-8 bf16).  With w_j the softmax weights, an output's error is at most
+  u |o| + (1.125 u + e) sum_j w_j |v_j|  (the result's rounding, the weights' rounding, and e, the relative error of a weight: twice the score's)
+plus, in fp16, what weights below its normal range lose.  Scores are sums of D products in fp32: 2 * 2^-23 * (D / 4) * sum |q k| scale."""
+import math
+
+import pytest
+import torch
+
+from tests.test_paged_cache import DEV, UNIT, _attention_case, _attention_reference
+
+
+# ---- capped scores: softcap tanh(s / softcap) ------------------------------------------------------------------------------------------
+#
+# The cap's own error is relative to the score.  From |x| = 1/5 on (x = s / softcap) tanh x is 1 - 2 / (e^2x + 1), whose last subtraction leaves at most
+# 13 * 2^-23 of the result for exp and reciprocal of an ulp each; below, a series, a few roundings.  16 * 2^-23 |score| covers both.
+
+def _check_capped(rtn, dtype, lens, softcap, D=128, scale=None, zero_query=False):
+    q, k, v, table, seq, start = _attention_case(dtype, lens, 4, 2, D, 16, seed=int(math.log10(softcap)) + 60)
+    if zero_query:
+        q[::2] = 0
+    out = torch.full(q.shape, float("nan"), dtype=dtype, device=DEV)
+    rtn.rtn_paged_attention(q, rtn.PagedCache(k, v), table, seq, start, max(n for _, n in lens), scale=scale, softcap=softcap, out=out)
+    s = D ** -0.5 if scale is None else scale
+    want, mass, _ = _attention_reference(q, k, v, table, lens, s, softcap, 0)
+    _, _, err = _attention_reference(q, k, v, table, lens, s, 0.0, 0)      # (the products' share, without the cap)
+    largest = float((q.double().abs().amax(0).sum(-1).max() * k.double().nan_to_num().abs().max()) * s)      # no score is above it
+    err = err + 2 * 16 * 2.0 ** -23 * min(softcap, largest)
+    u = UNIT[dtype]
+    bound = 1.01 * u * want.abs() + (1.125 * u + err) * mass + 2.0 ** -24
+    assert torch.isfinite(out).all()
+    for exact in [want] + ([_attention_reference(q, k, v, table, lens, s, 0.0, 0)[0]] if softcap >= 1e8 else []):     # (from there on the cap is none)
+        over = (out.cpu().double() - exact).abs() - bound
+        assert (over <= 0).all(), float(over.max())
+
+
+CAPPED = {"decode": [(6, 1), (0, 1), (40, 1)], "drafts": [(3, 9), (17, 4)], "tiles": [(5, 70), (0, 40), (33, 1)]}
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", sorted(CAPPED))
+@pytest.mark.parametrize("softcap", [1e3, 1e4, 1e5, 1e6, 1e8, 1e20, 1e38])
+def test_large_caps_are_as_exact_as_none(rtn, lens, softcap):
+    for dtype, D in ((torch.float16, 128), (torch.float16, 64), (torch.bfloat16, 256)):
+        _check_capped(rtn, dtype, CAPPED[lens], softcap, D)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", sorted(CAPPED))
+@pytest.mark.parametrize("softcap", [1e-45, 1e-39, 1e-30, 1e-3, 0.3, 2.0])
+def test_small_caps(rtn, lens, softcap):
+    """Down to the smallest that fp32 has, where scale / softcap is beyond its range; a score of zero stays zero."""
+    for dtype, D in ((torch.float16, 128), (torch.float16, 64), (torch.bfloat16, 256)):
+        _check_capped(rtn, dtype, CAPPED[lens], softcap, D, zero_query=True)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", sorted(CAPPED))
+def test_scores_across_the_cap(rtn, lens):
+    """Scores from far below to far above the cap, through the change of formula."""
+    for softcap, scale in ((4.0, 0.5), (20.0, 1.0), (50.0, 2.0)):
+        _check_capped(rtn, torch.float16, CAPPED[lens], softcap, 64, scale=scale)
