@@ -55,6 +55,11 @@ __device__ __forceinline__ float capped(const AttnParams& p, float s) {
     return fabsf(z) < limit ? small : large;
 }
 
+// Weights of V go to the matrix cores in the element type.  fp16 has normal numbers from 2^-14 to 2^16 only, and a long cache whose largest score is far above the others
+// has its sum in weights below that: they are multiplied by a power of two that takes the largest possible one to 2^15.  The sums carry it too, so it divides out.
+// (bf16 has fp32's range.)
+template <int TYPE> constexpr float weight_lift(float most) { return TYPE == RTN_TYPE_F16 ? 15.0f - most : 0.0f; }      // log2; `most`: that of the largest weight
+
 // What a workgroup does: ROWS rows from row0 of request b, a part of their keys.
 struct Piece {
     int b, row0, rows, tok0, n, ctx;                         // rows of the tile, first token in the batch, new tokens, cached tokens
@@ -412,13 +417,13 @@ __device__ __forceinline__ void attend_few(const AttnParams& p, int block, uint8
             for (int j = 0; j < 8; ++j) top = fmaxf(top, e[j]);
             top = fmaxf(top, __shfl_xor(top, 16));
             top = fmaxf(top, __shfl_xor(top, 32));
-            const float m_new = fmaxf(m[n], top), base = m_new == -INFINITY ? 0.f : m_new;
+            const float m_new = fmaxf(m[n], top), base = m_new == -INFINITY ? 0.f : m_new, from = base - weight_lift<TYPE>(0.f);
             back[n] = exp2_of(m[n] - base);
             m[n] = m_new;
             l[n] *= back[n];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const float x = exp2_of(e[j] - base);
+                const float x = exp2_of(e[j] - from);
                 l[n] += x;
                 pt[n][j] = (T)x;
                 if constexpr (REST) rest[n][j] = (T)(x - (float)pt[n][j]);
@@ -655,9 +660,10 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
 #pragma unroll
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[h][j]);
         top = fmaxf(top, __shfl_xor(top, 32)) * scale;
-        // The weights are relative to a maximum that is only followed where it has grown by 2^8: they stay below 2^8, exact to the same share, and the
-        // sums, most of the time, need no rescaling.
-        if (__any(top > m + 8.f)) {
+        // The weights are relative to a maximum that is only followed where it has grown by 2^kLag: they stay below that, exact to the same share, and the
+        // sums, most of the time, need no rescaling.  (fp16 keeps more of its range for small weights.)
+        constexpr float kLag = TYPE == RTN_TYPE_F16 ? 4.f : 8.f;
+        if (__any(top > m + kLag)) {
             const float m_new = fmaxf(m, top), back = m_new == -INFINITY ? 1.f : exp2_of(m - m_new);
             m = m_new;
             l *= back;
@@ -666,7 +672,7 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[t][j] *= back;
         }
-        const float base = m == -INFINITY ? 0.f : m;
+        const float base = (m == -INFINITY ? 0.f : m) - weight_lift<TYPE>(kLag);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int h = 0; h < KT * 2; ++h) {

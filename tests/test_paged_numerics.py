@@ -62,3 +62,35 @@ def test_scores_across_the_cap(rtn, lens):
     """Scores from far below to far above the cap, through the change of formula."""
     for softcap, scale in ((4.0, 0.5), (20.0, 1.0), (50.0, 2.0)):
         _check_capped(rtn, torch.float16, CAPPED[lens], softcap, 64, scale=scale)
+
+
+# ---- weights far below the largest -----------------------------------------------------------------------------------------------------
+#
+# One key that takes nearly all the weight, with a V of zero, before n like ones with V of one: the result is what the small weights come to.  In fp16
+# the weights are multiplied by 2^15 (few rows) or, whose weights may be 2^4 times those of the largest score yet seen, by 2^11 (many rows): a weight has
+# an error of u of itself, or 2^-25 below the normal range, 2^-40 or 2^-36 of the largest.
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [torch.float16, torch.bfloat16])
+@pytest.mark.parametrize("D", [64, 128, 256])
+@pytest.mark.parametrize("new,lost", [(1, 40), (7, 40), (70, 36)])
+@pytest.mark.parametrize("split", [False, True])
+@pytest.mark.parametrize("nats", [5.0, 14.0, 15.0, 16.0, 17.0, 18.0])
+def test_many_small_weights_beside_a_large_one(rtn, dtype, D, new, lost, split, nats):
+    """In one piece, all of them beside the large one, and split, where every part has a maximum of its own."""
+    n, ps, Hq = 32768, 256, 4
+    pages = -(-(n + new) // ps)
+    k, v = (torch.full((pages, 1, ps, D), x, dtype=dtype, device=DEV) for x in (0.0, 1.0))
+    k[0, 0, 0], v[0, 0, 0] = 1.0, 0.0
+    q = torch.ones(new, Hq, D, dtype=dtype, device=DEV)
+    table = torch.arange(pages, dtype=torch.int32, device=DEV)[None]
+    seq, start = (torch.tensor(x, dtype=torch.int32, device=DEV) for x in ([n + new], [0, new]))
+    out = rtn.rtn_paged_attention(q, rtn.PagedCache(k, v), table, seq, start, new, scale=nats / D,
+                                  workspace=None if split else torch.empty(0, dtype=torch.uint8, device=DEV))
+    small = torch.arange(n, n + new, dtype=torch.float64) * math.exp(-nats)        # the token at position p sees p like keys
+    want = (small / (1 + small))[:, None, None]
+    u = UNIT[dtype]
+    e = 4 * 2.0 ** -23 * (D / 4) * nats + 2.0 ** -20
+    bound = (1.01 * u + 1.125 * u + e) * want + (0.0 if dtype is torch.bfloat16 else (n + new) * 2.0 ** -lost + 2.0 ** -25)
+    over = ((out.cpu().double() - want).abs() / bound).max()
+    assert over <= 1, (float(over), float(out.float().mean()), float(want.mean()))
