@@ -887,14 +887,15 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     int few_most, few_slots, many_most, many_slots;
     bounds(few_tiles, a.few, rtn::few_keys(a.mixed ? 8 : 4), &few_most, &few_slots);
     bounds(many_tiles, a.many, rtn::tile_keys(D), &many_most, &many_slots);
-    const float log2e = 1.4426950408889634f;
     float* const ws = static_cast<float*>(dev_workspace);
-    // (a cap so small that this passes fp32's range: scores of zero stay zero, all others are at the cap either way)
-    const float cap_in = softcap > 0.f ? (float)std::min(2.0 * scale / softcap * 1.4426950408889634, (double)FLT_MAX) : 0.f;
+    // Factors that would pass fp32's range become its largest number: a score of zero stays zero.  (With a cap so small that its factor does, all others are at the cap either way.)
+    auto finite = [](double x) { return (float)std::min(x, (double)FLT_MAX); };
+    const double log2e = 1.4426950408889634;
+    const float cap_in = softcap > 0.f ? finite(2.0 * scale / softcap * log2e) : 0.f;
     const rtn::AttnParams p = {dev_q, cache->dev_k, cache->dev_v, dev_out, dev_block_table, dev_seq_lens, dev_query_start, q_stride, cache->page_stride,
                                cache->head_stride, cache->token_stride, table_stride, (int)cache->pages, rtn::log2_of(cache->page_size), max_blocks,
-                               n_requests, (int)tokens, q_heads, Hk, G, window, scale * log2e, softcap, cap_in,
-                               softcap * log2e, G == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / G) + 1, G == 1 ? 0xFFFFFFFFu : 0u, a.mixed ? rtn::kFew : 0x7FFFFFFF, {ws + tiles_bytes / 4, a.few, few_most, few_slots}, {ws, a.many, many_most, many_slots}};
+                               n_requests, (int)tokens, q_heads, Hk, G, window, finite(scale * log2e), softcap, cap_in,
+                               finite(softcap * log2e), G == 1 ? 0u : (uint32_t)(((uint64_t)1 << 32) / G) + 1, G == 1 ? 0xFFFFFFFFu : 0u, a.mixed ? rtn::kFew : 0x7FFFFFFF, {ws + tiles_bytes / 4, a.few, few_most, few_slots}, {ws, a.many, many_most, many_slots}};
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (cache->dtype == RTN_TYPE_F16) {
         if (D == 64) rtn::launch_attention<RTN_TYPE_F16, 64>(p, a, s);

@@ -94,3 +94,18 @@ def test_many_small_weights_beside_a_large_one(rtn, dtype, D, new, lost, split, 
     bound = (1.01 * u + 1.125 * u + e) * want + (0.0 if dtype is torch.bfloat16 else (n + new) * 2.0 ** -lost + 2.0 ** -25)
     over = ((out.cpu().double() - want).abs() / bound).max()
     assert over <= 1, (float(over), float(out.float().mean()), float(want.mean()))
+
+
+# ---- scale ---------------------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("lens", sorted(CAPPED))
+@pytest.mark.parametrize("softcap", [0.0, 3e38])
+def test_largest_scale_with_scores_of_zero(rtn, lens, softcap):
+    """A scale, or a cap, that fp32 holds and its product with log2 e does not: scores of zero are zero, the result the mean of what is seen."""
+    q, k, v, table, seq, start = _attention_case(torch.float16, CAPPED[lens], 4, 2, 128, 16)
+    q.zero_()
+    out = rtn.rtn_paged_attention(q, rtn.PagedCache(k, v), table, seq, start, max(n for _, n in CAPPED[lens]), scale=3.4e38, softcap=softcap)
+    want, mass, _ = _attention_reference(q, k, v, table, CAPPED[lens], 1.0, 0.0, 0)
+    u = UNIT[torch.float16]
+    assert ((out.cpu().double() - want).abs() <= 1.01 * u * want.abs() + (1.125 * u + 2.0 ** -20) * mass + 2.0 ** -24).all()
