@@ -342,8 +342,9 @@ typedef struct {
  *   dev_positions, dev_slots   out  int32 [max_tokens]: of new token query_start[b] + i: cached_lens[b] + i, and page * page_size + offset;
  *                     -1 from query_start[n_requests] on
  *   dev_free_count_out, dev_status   out  int32 [1]
- * status: 0, or what does not fit, as a sum of 1 (pages), 2 (a row of the table), 4 (max_tokens), 8 (a length or count out of range:
- * cached_lens, free_count, or more pages back than the stack has entries).  Then nothing happens: lengths and count stay, query_start is 0,
+ * status: 0, or everything that does not fit, as a sum of 1 (more pages needed than free_count says and come back), 2 (a row of the table), 4 (max_tokens),
+ * 8 (a length or count out of range: cached_lens, free_count, or more pages back, or free after the step, than the stack has entries); the pages and tokens of
+ * requests that 2, 4 or 8 says of by themselves are not counted for 1 and 4.  Then nothing happens: lengths and count stay, query_start is 0,
  * positions and slots -1, table and stack are untouched.
  * dev_seq_lens may be dev_cached_lens and dev_free_count_out may be dev_free_count, as a loop of replays wants it; no other buffers may
  * overlap.  n_requests 1 .. 4096, max_tokens below 2^30, pool up to 2^27. */

@@ -57,13 +57,13 @@ __device__ __forceinline__ Request read_request(const PlanParams& p, int b) {
 __global__ __launch_bounds__(1024) void cache_plan_kernel(const PlanParams p) {
     extern __shared__ int lds[];
     __shared__ int part[16][4];
-    __shared__ float large[16][3];
+    __shared__ int high[16][3];
     int *const ends = lds, *const pops = ends + p.B, *const frees = pops + p.B, *const cached = frees + p.B;
     const int tid = threadIdx.x, threads = blockDim.x, lane = tid & 63, wave = tid >> 6, waves = threads >> 6;
     const int count = *p.count;
 
-    // Each thread's requests, then the sums before it: within the wavefront, then over the wavefronts.  32 bits hold every sum that is used:
-    // one that they do not hold is seen by its sum in fp32, and is more than there can be.
+    // Each thread's requests, then the sums before it: within the wavefront, then over the wavefronts.  32 bits hold every sum that is used; what the whole batch
+    // comes to is known exactly, from the sum of the numbers' upper parts beside it.
     const int per = (p.B + threads - 1) / threads, b0 = min(p.B, tid * per), b1 = min(p.B, b0 + per);
     constexpr int KEEP = 4;                                  // read at once and kept: up to 1024 requests of 256 threads
     Request own[KEEP];
@@ -76,28 +76,28 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(const PlanParams p) {
         for (int b = b0 + KEEP; b < b1; ++b) f(b, read_request(p, b));
     };
     uint32_t sum[3] = {0, 0, 0};
-    float about[3] = {0.f, 0.f, 0.f};
+    int upper[3] = {0, 0, 0};                                // of 16 bits and above: below 2^26 in all, and what is left of the sum below 2^28
     int flags = 0;
     each([&](int, const Request& r) {
         sum[0] += r.tokens;
         sum[1] += r.need;
         sum[2] += r.freed;
-        about[0] += (float)r.tokens;
-        about[1] += (float)r.need;
-        about[2] += (float)r.freed;
+        upper[0] += r.tokens >> 16;
+        upper[1] += r.need >> 16;
+        upper[2] += r.freed >> 16;
         flags |= r.flags;
     });
     uint32_t before[3], total[3] = {0, 0, 0};
-    float most[3] = {0.f, 0.f, 0.f};
+    int above[3] = {0, 0, 0};
     flags = (__any(flags & 1) ? 1 : 0) | (__any(flags & 2) ? 2 : 0) | (__any(flags & 4) ? 4 : 0) | (__any(flags & 8) ? 8 : 0);
 #pragma unroll
     for (int k = 0; k < 3; ++k) {
         const uint32_t s = wave_scan(sum[k]);
-        const float f = wave_scan(about[k]);
+        const int u = wave_scan(upper[k]);
         before[k] = s - sum[k];
         if (lane == 63) {
             part[wave][k] = s;
-            large[wave][k] = f;
+            high[wave][k] = u;
         }
     }
     if (lane == 63) part[wave][3] = flags;
@@ -108,15 +108,15 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(const PlanParams p) {
         for (int k = 0; k < 3; ++k) {
             if (w < wave) before[k] += part[w][k];
             total[k] += part[w][k];
-            most[k] += large[w][k];
+            above[k] += high[w][k];
         }
         flags |= part[w][3];
     }
-    const int64_t left = (int64_t)count + total[2] - total[1];
-    if (count < 0 || count > p.pool || most[2] > 0x1p29f || total[2] > (uint64_t)p.pool) flags |= 8;
-    else if (most[1] > 0x1p30f || left < 0) flags |= 1;      // (count and what comes back are 2^28 at most)
-    else if (left > p.pool) flags |= 8;
-    if (most[0] > 0x1.01p30f || total[0] > (uint32_t)p.max_tokens) flags |= 4;
+    auto whole = [&](int k) { return ((int64_t)above[k] << 16) + (uint32_t)(total[k] - ((uint32_t)above[k] << 16)); };
+    const int64_t back = whole(2), left = count + back - whole(1);
+    if (count < 0 || count > p.pool || back > p.pool || left > p.pool) flags |= 8;
+    if (left < 0) flags |= 1;
+    if (whole(0) > p.max_tokens) flags |= 4;
 
     // (where flags are set, the sums are not used)
     each([&](int b, const Request& r) {

@@ -6,10 +6,11 @@ u is the unit roundoff of the element type (2^-11 fp16, 2^-8 bf16).  With w_j th
 plus, in fp16, what weights below its normal range lose.  Scores are sums of D products in fp32: 2 * 2^-23 * (D / 4) * sum |q k| scale."""
 import math
 
+import numpy as np
 import pytest
 import torch
 
-from tests.test_paged_cache import DEV, UNIT, _attention_case, _attention_reference
+from tests.test_paged_cache import DEV, UNIT, _attention_case, _attention_reference, _plan_case, _plan_reference, _run_plan, _same_plan
 
 
 # ---- capped scores: softcap tanh(s / softcap) ------------------------------------------------------------------------------------------
@@ -109,3 +110,43 @@ def test_largest_scale_with_scores_of_zero(rtn, lens, softcap):
     want, mass, _ = _attention_reference(q, k, v, table, CAPPED[lens], 1.0, 0.0, 0)
     u = UNIT[torch.float16]
     assert ((out.cpu().double() - want).abs() <= 1.01 * u * want.abs() + (1.125 * u + 2.0 ** -20) * mass + 2.0 ** -24).all()
+
+
+# ---- the plan's status -----------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("what", ["negative", "most_negative", "above", "far_above", "all"])
+def test_plan_says_everything_that_does_not_fit(rtn, what, in_place):
+    """The bits of the status do not depend on one another: a free count out of range, and too few pages for the step."""
+    step, cached, table, free, count, ps, max_tokens = _plan_case(11, 40, 16, 20, 200, 60, 0.2, 3)
+    step = np.where(step < 0, 1, step).astype(np.int32)        # (nothing comes back)
+    if what == "negative":
+        count = -1
+    elif what == "most_negative":
+        count = -2 ** 31
+    elif what == "above":                                     # a stack of three, said to hold four, for a step that needs more
+        free, count = free[:3].copy(), 4
+    elif what == "far_above":
+        count = 2 ** 31 - 1
+    else:
+        count, cached[7], step[9], max_tokens = -5, -3, 2 ** 30, 7
+    case = (step, cached, table, free, count, ps, max_tokens)
+    want = _plan_reference(*case)
+    assert want[5] & 8 and bool(want[5] & 1) == (what != "far_above")
+    _same_plan(_run_plan(case, in_place), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("back,need,status", [(0, 4096, 1 | 4), (4096, 0, 8), (2048, 2048, 8 | 1 | 4), (4095, 1, 8)])
+def test_plan_sums_that_pass_32_bits(rtn, back, need, status):
+    """4096 requests of 2^20 + 4 pages: the pages given back or needed come to 2^32 + 16384, which is not 16384."""
+    B, ps, blocks = 4096, 16, 2 ** 20 + 8
+    ends = torch.arange(B, device=DEV) < back
+    cached = torch.where(ends, 2 ** 24 + 64, 0).to(torch.int32)
+    step = torch.where(ends, -1, 2 ** 24 + 128 if back else 2 ** 24 + 64).to(torch.int32)
+    table = torch.empty(B, blocks, dtype=torch.int32, device=DEV)
+    free, count, lens = torch.zeros(30000, dtype=torch.int32, device=DEV), torch.tensor([100 if back else 20000], dtype=torch.int32, device=DEV), cached.clone()
+    plan = rtn.rtn_cache_plan(step, lens, table, free, count, ps, 2 ** 25)
+    assert back + need == B and int(plan.status) == status
+    assert torch.equal(plan.seq_lens, cached) and int(plan.free_count) == int(count) and not plan.query_start.any() and (plan.slots == -1).all()
