@@ -171,6 +171,12 @@ def _dev_fp16(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a contiguous fp16 CUDA matrix")
 
 
+def _dev_workspace(t: torch.Tensor, device: torch.device):
+    """One piece of memory on the GPU that the call runs on: kernels write anywhere in its bytes."""
+    if not (t.is_cuda and t.is_contiguous() and t.device == device):
+        raise ValueError("workspace must be a contiguous CUDA tensor on the call's device")
+
+
 def rtn_layout_version() -> int:
     return _lib.rtn_layout_version()
 
@@ -579,6 +585,7 @@ def rtn_paged_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.T
     if workspace is None:
         need = _lib.rtn_paged_attention_workspace_nbytes(T, B, Hq, cache._ref, max_new)
         workspace = torch.empty(max(need, 16), dtype=torch.uint8, device=q.device)
+    _dev_workspace(workspace, q.device)
     _check(_lib.rtn_paged_attention(q.data_ptr(), T, _row_stride(q), Hq, cache._ref, block_table.data_ptr(), _row_stride(block_table), block_table.shape[1],
                                     seq_lens.data_ptr(), query_start.data_ptr(), B, max_new, D ** -0.5 if scale is None else scale, softcap, window,
                                     out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream()), "rtn_paged_attention")

@@ -212,7 +212,8 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
         if (!x.is_cuda() || x.scalar_type() != type || x.dim() != 3 || x.size(2) != c->head_dim || x.stride(2) != 1 || x.size(1) > INT32_MAX) Py_RETURN_NONE;
         T = x.size(0); H = x.size(1);
         if (H != 1 && x.stride(1) != x.size(2)) Py_RETURN_NONE;
-        if (!y.is_cuda() || y.scalar_type() != type || y.sizes() != x.sizes() || !y.is_contiguous() || !w.is_cuda()) Py_RETURN_NONE;
+        if (!y.is_cuda() || y.scalar_type() != type || y.sizes() != x.sizes() || !y.is_contiguous()) Py_RETURN_NONE;
+        if (!w.is_cuda() || !w.is_contiguous() || w.device() != x.device()) Py_RETURN_NONE;
         if (!ints(a[3], -1, &seq, &B) || B > INT32_MAX - 1 || !ints(a[4], B + 1, &start) || !table(a[2], B, &tab, &stride, &width)) Py_RETURN_NONE;
         q = x.data_ptr(); out = y.data_ptr(); ws = w.data_ptr();
         qs = row_stride(x); bytes = w.nbytes();

@@ -150,3 +150,57 @@ def test_plan_sums_that_pass_32_bits(rtn, back, need, status):
     plan = rtn.rtn_cache_plan(step, lens, table, free, count, ps, 2 ** 25)
     assert back + need == B and int(plan.status) == status
     assert torch.equal(plan.seq_lens, cached) and int(plan.free_count) == int(count) and not plan.query_start.any() and (plan.slots == -1).all()
+
+
+# ---- workspaces ----------------------------------------------------------------------------------------------------------------------
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on the GPU: the binding's checks run without one."""
+    is_cuda = property(lambda self: True)
+
+
+def _on_gpu(*shape, dtype=torch.float16):
+    return torch.zeros(*shape, dtype=dtype).as_subclass(OnGpu)
+
+
+@pytest.fixture
+def launches(monkeypatch):
+    """The binding without a GPU and without native code: what would have been launched, none of it launched."""
+    from paper_2505_15909_amd import binding
+    seen = []
+
+    class Library:
+        def __getattr__(self, name):
+            return getattr(real, name) if name.endswith("nbytes") else lambda *a: seen.append((name, a)) or 0
+
+    real = binding._lib
+    monkeypatch.setattr(binding, "_lib", Library())
+    monkeypatch.setattr(binding, "_native", None)
+    monkeypatch.setattr(binding, "_stream", lambda: 0)
+    return seen
+
+
+WORKSPACES = {"on the host": lambda t: torch.zeros(4096, dtype=torch.uint8), "strided": lambda t: t(4096, dtype=torch.uint8)[::2],
+              "expanded": lambda t: t(1, dtype=torch.uint8).expand(1 << 20), "transposed": lambda t: t(64, 64, dtype=torch.float32).t()}
+
+
+@pytest.mark.parametrize("what", sorted(WORKSPACES))
+def test_attention_refuses_a_workspace_that_is_not_one_piece_on_the_gpu(launches, what):
+    import paper_2505_15909_amd as rtn
+    q, ints = _on_gpu(2, 4, 128), lambda *n: _on_gpu(*n, dtype=torch.int32)
+    cache = rtn.PagedCache(_on_gpu(4, 2, 16, 128), _on_gpu(4, 2, 16, 128))
+    for out in (None, _on_gpu(2, 4, 128)):
+        with pytest.raises(ValueError, match="workspace"):
+            rtn.rtn_paged_attention(q, cache, ints(2, 3), ints(2), ints(3), 1, out=out, workspace=WORKSPACES[what](_on_gpu))
+    assert not launches
+    rtn.rtn_paged_attention(q, cache, ints(2, 3), ints(2), ints(3), 1, out=q, workspace=_on_gpu(4096, dtype=torch.uint8))
+    assert [name for name, _ in launches] == ["rtn_paged_attention"]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("what", sorted(WORKSPACES))
+def test_native_attention_leaves_such_a_workspace_to_be_refused(rtn, what):
+    q, k, v, table, seq, start = _attention_case(torch.float16, CAPPED["drafts"], 4, 2, 128, 16)
+    with pytest.raises(ValueError, match="workspace"):
+        rtn.rtn_paged_attention(q, rtn.PagedCache(k, v), table, seq, start, 9, out=torch.empty_like(q),
+                                workspace=WORKSPACES[what](lambda *n, dtype: torch.zeros(*n, dtype=dtype, device=DEV)))
