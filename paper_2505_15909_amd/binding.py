@@ -171,10 +171,10 @@ def _dev_fp16(t: torch.Tensor, name: str):
         raise ValueError(f"{name} must be a contiguous fp16 CUDA matrix")
 
 
-def _dev_workspace(t: torch.Tensor, device: torch.device):
+def _dev_workspace(t: torch.Tensor, device: torch.device, name: str = "workspace"):
     """One piece of memory on the GPU that the call runs on: kernels write anywhere in its bytes."""
     if not (t.is_cuda and t.is_contiguous() and t.device == device):
-        raise ValueError("workspace must be a contiguous CUDA tensor on the call's device")
+        raise ValueError(f"{name} must be a contiguous CUDA tensor on the call's device")
 
 
 def rtn_layout_version() -> int:
@@ -236,6 +236,7 @@ def rtn_linear(A: torch.Tensor, qweight: torch.Tensor, scales: torch.Tensor, bit
     if workspace is None:
         workspace = torch.empty(max(256, _lib.rtn_workspace_nbytes(M, N, K, bits, group_size)),
                                 dtype=torch.uint8, device=A.device)
+    _dev_workspace(workspace, A.device)
     c = make_cfg(cfg)
     st = _lib.rtn_linear_ex(A.data_ptr(), M, qweight.data_ptr(), scales.data_ptr(), N, K, bits, group_size,
                             out.data_ptr(), workspace.data_ptr(), workspace.nbytes,
@@ -326,6 +327,8 @@ def rtn_gemm_fp16(A: torch.Tensor, W: torch.Tensor, out: torch.Tensor = None, wo
     N = W.shape[0]
     if out is None:
         out = torch.empty((M, N), dtype=torch.float16, device=A.device)
+    if workspace is not None:
+        _dev_workspace(workspace, A.device)
     wp, wn = (workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0)
     _check(_lib.rtn_gemm_fp16(A.data_ptr(), M, W.data_ptr(), N, K, out.data_ptr(), wp, wn, _stream()), "rtn_gemm_fp16")
     return out
@@ -339,6 +342,9 @@ def rtn_linear_dense(A: torch.Tensor, qweight: torch.Tensor, scales: torch.Tenso
     N = scales.shape[0]
     if out is None:
         out = torch.empty((M, N), dtype=torch.float16, device=A.device)
+    _dev_workspace(w_tmp, A.device, "w_tmp")
+    if workspace is not None:
+        _dev_workspace(workspace, A.device)
     wp, wn = (workspace.data_ptr(), workspace.nbytes) if workspace is not None else (None, 0)
     _check(_lib.rtn_linear_dense(A.data_ptr(), M, qweight.data_ptr(), scales.data_ptr(), N, K, bits, group_size,
                                  out.data_ptr(), w_tmp.data_ptr(), w_tmp.numel() * w_tmp.element_size(), wp, wn,
@@ -367,6 +373,8 @@ class LayerPlan:
             need = max(need, _lib.rtn_workspace_nbytes(M, N, K, m["bits"], m["group_size"]))
         if workspace is None:
             workspace = torch.empty(need, dtype=torch.uint8, device=modules[0]["A"].device)
+        if modules:
+            _dev_workspace(workspace, modules[0]["A"].device)
         self.workspace = workspace
 
     def run(self):
@@ -421,6 +429,7 @@ def rtn_linear_asym(A, qweight, scales, zeros, bits, group_size, out=None, works
     if workspace is None:
         workspace = torch.empty(max(256, _lib.rtn_workspace_nbytes(M, N, K, bits, group_size)), dtype=torch.uint8,
                                 device=A.device)
+    _dev_workspace(workspace, A.device)
     _check(_lib.rtn_linear_asym(A.data_ptr(), M, qweight.data_ptr(), scales.data_ptr(), zeros.data_ptr(), N, K, bits,
                                 group_size, out.data_ptr(), workspace.data_ptr(), workspace.numel(), _stream()),
            "rtn_linear_asym")

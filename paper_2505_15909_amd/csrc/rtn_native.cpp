@@ -46,6 +46,7 @@ PyObject* call(PyObject* const* args, bool zp) {
         const at::Tensor &a = THPVariable_Unpack(pa), &q = THPVariable_Unpack(pq), &s = THPVariable_Unpack(ps), &c = THPVariable_Unpack(pc),
                          &w = THPVariable_Unpack(pw);
         if (!a.is_cuda() || a.scalar_type() != at::kHalf || a.dim() != 2 || !a.is_contiguous() || s.dim() < 1) Py_RETURN_NONE;
+        if (!w.is_cuda() || !w.is_contiguous() || w.device() != a.device()) Py_RETURN_NONE;
         da = a.data_ptr(); dq = q.data_ptr(); ds = s.data_ptr(); dc = c.data_ptr(); dw = w.data_ptr();
         if (zp) dz = THPVariable_Unpack(pz).data_ptr();
         M = a.size(0); K = a.size(1); N = s.size(0);
