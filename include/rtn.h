@@ -365,7 +365,7 @@ rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev_cached_len
  *   dev_positions, dev_slots   in   int32 [tokens]; two tokens of a call must not have the same slot
  *   dev_q_norm, dev_k_norm     in   [head_dim] in the cache's type, or NULL: no norm
  *   dev_q_out      out  [tokens, q_heads, head_dim]
- * tokens 0 .. 2^24 (0: nothing to do), tokens * (q_heads + 2 kv_heads) below 2^31. */
+ * tokens 0 .. 2^24 (0: nothing to do), tokens * (q_heads + 2 kv_heads) * head_dim at most 2^35 - 2^11 (a launch's threads). */
 rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_t qkv_stride, int q_heads, const float* dev_rope, int rotary_dim,
                           int64_t max_positions, int interleaved, const int32_t* dev_positions, const int32_t* dev_slots,
                           const void* dev_q_norm, const void* dev_k_norm, float eps, const rtn_kv_cache* cache, void* dev_q_out, void* stream);
@@ -385,8 +385,9 @@ rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_t qkv_strid
  *   dev_out        out  [tokens, q_heads, head_dim]
  *   dev_workspace  scratch, rtn_paged_attention_workspace_nbytes() bytes; with less or NULL long requests are not split over
  *                  workgroups (slower, not an error); contents undefined before and after; calls that overlap in time need distinct ones
- * q_heads a multiple of kv_heads, up to 64 times as many; tokens 0 .. 2^20; n_requests 1 .. 65536.  The same inputs with the same
- * workspace size give the same bits. */
+ * q_heads a multiple of kv_heads, up to 64 times as many; tokens 0 .. 2^20; n_requests 1 .. 65536; no more tiles of rows than a launch has threads for
+ * (tokens * q_heads up to 2^26 and n_requests * kv_heads up to 2^20 always fit; RTN_ERR_SHAPE otherwise, where they do not).  The same inputs with the
+ * same workspace size give the same bits. */
 size_t rtn_paged_attention_workspace_nbytes(int64_t tokens, int n_requests, int q_heads, const rtn_kv_cache* cache, int max_new);
 rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int64_t q_stride, int q_heads, const rtn_kv_cache* cache,
                                const int32_t* dev_block_table, int64_t table_stride, int max_blocks, const int32_t* dev_seq_lens,

@@ -875,7 +875,6 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     const int64_t rows = tokens * G;
     const int64_t few_tiles = std::min(rows / a.rows + n_requests, a.mixed ? (int64_t)n_requests * (rtn::kFew / a.rows) : rows);
     const int64_t many_tiles = a.mixed ? rows / rtn::kTileRows + std::min<int64_t>(n_requests, rows / rtn::kFew) : 0;
-    if ((few_tiles + a.few + many_tiles + a.many) * Hk >= 0x7FFFFFFF) return RTN_ERR_SHAPE;
     auto bounds = [&](int64_t tiles, int pieces, int keys, int* most, int* slots) {
         const int64_t parts = ((int64_t)max_blocks * cache->page_size + keys - 1) / keys;     // of the longest request that the table holds
         *most = (int)std::min(tiles + pieces, tiles * parts);
@@ -887,6 +886,7 @@ extern "C" rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int
     int few_most, few_slots, many_most, many_slots;
     bounds(few_tiles, a.few, rtn::few_keys(a.mixed ? 8 : 4), &few_most, &few_slots);
     bounds(many_tiles, a.many, rtn::tile_keys(D), &many_most, &many_slots);
+    if (!rtn::launchable(((int64_t)few_most + many_most) * Hk, a.mixed ? 512 : 256)) return RTN_ERR_SHAPE;      // (the join's launch is far smaller)
     float* const ws = static_cast<float*>(dev_workspace);
     // Factors that would pass fp32's range become its largest number: a score of zero stays zero.  (With a cap so small that its factor does, all others are at the cap either way.)
     auto finite = [](double x) { return (float)std::min(x, (double)FLT_MAX); };

@@ -195,7 +195,7 @@ __global__ __launch_bounds__(256) void rope_cache_kernel(const RopeParams p) {
     typedef typename Elem<TYPE>::x4 T4;
     constexpr int L = D / 8;                                 // lanes of a head
     const int H = p.Hq + 2 * p.Hk;
-    const uint32_t row = blockIdx.x * (256 / L) + threadIdx.x / L;       // (below 2^31 + 32)
+    const uint32_t row = blockIdx.x * (256 / L) + threadIdx.x / L;       // (below 2^29: a launch has fewer than 2^32 threads)
     const int c = threadIdx.x % L;
     if (row >= (uint32_t)(p.tokens * H)) return;             // (whole heads: the lanes of one stay together)
     const int t = (int)(row / (uint32_t)H), h = (int)(row - (uint32_t)t * H);
@@ -251,10 +251,11 @@ __global__ __launch_bounds__(256) void rope_cache_kernel(const RopeParams p) {
     __builtin_nontemporal_store(y1, reinterpret_cast<T4*>(dst + e1));
 }
 
+static int64_t rope_blocks(int64_t tokens, int heads, int D) { return (tokens * heads * (D / 8) + 255) / 256; }
+
 template <int TYPE, int D>
 static void launch_rope(const RopeParams& p, bool interleaved, hipStream_t st) {
-    const int64_t rows = (int64_t)p.tokens * (p.Hq + 2 * p.Hk), per = 256 / (D / 8);
-    const dim3 grid((unsigned)((rows + per - 1) / per));
+    const dim3 grid((unsigned)rope_blocks(p.tokens, p.Hq + 2 * p.Hk, D));
     if (interleaved) hipLaunchKernelGGL((rope_cache_kernel<TYPE, D, true>), grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL((rope_cache_kernel<TYPE, D, false>), grid, dim3(256), 0, st, p);
 }
@@ -304,7 +305,7 @@ extern "C" rtn_status rtn_rope_cache(const void* dev_qkv, int64_t tokens, int64_
         !rtn::aligned_to(dev_k_norm, 16) || !rtn::aligned_to(dev_q_out, 16) || !rtn::aligned_to(dev_positions, 4) || !rtn::aligned_to(dev_slots, 4))
         return RTN_ERR_ALIGN;
     if (!(eps >= 0.f) || (interleaved != 0 && interleaved != 1)) return RTN_ERR_CONFIG;
-    if (tokens * (q_heads + 2 * cache->kv_heads) > 0x7FFFFFFF) return RTN_ERR_SHAPE;
+    if (!rtn::launchable(rtn::rope_blocks(tokens, q_heads + 2 * cache->kv_heads, D), 256)) return RTN_ERR_SHAPE;
     if (tokens == 0) return RTN_OK;
     const rtn::RopeParams p = {dev_qkv, dev_q_norm, dev_k_norm, dev_rope, dev_positions, dev_slots, dev_q_out, cache->dev_k, cache->dev_v, qkv_stride,
                                cache->page_stride, cache->head_stride, cache->token_stride, max_positions, cache->pages * cache->page_size, (int)tokens,

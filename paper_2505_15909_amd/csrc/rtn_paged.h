@@ -66,6 +66,9 @@ inline bool aligned_to(const void* p, unsigned n) { return (reinterpret_cast<uin
 
 inline bool page_size_valid(int ps) { return ps >= 16 && ps <= 256 && (ps & (ps - 1)) == 0; }
 
+// A launch's threads are counted in 32 bits.
+inline bool launchable(int64_t workgroups, int threads) { return workgroups <= (int64_t)UINT32_MAX / threads; }
+
 inline int log2_of(int pow2) { return 31 - __builtin_clz((unsigned)pow2); }
 
 // Strides of whole 16-byte pieces; a page's heads and tokens are addressed with 32 bits from its start.

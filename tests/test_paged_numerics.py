@@ -10,7 +10,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_paged_cache import DEV, UNIT, _attention_case, _attention_reference, _plan_case, _plan_reference, _run_plan, _same_plan
+from tests.test_paged_cache import DEV, SHAPE, UNIT, _attend, _attention_case, _attention_reference, _cache, _plan_case, _plan_reference, _rope, _run_plan, _same_plan, lib
 
 
 # ---- capped scores: softcap tanh(s / softcap) ------------------------------------------------------------------------------------------
@@ -204,3 +204,20 @@ def test_native_attention_leaves_such_a_workspace_to_be_refused(rtn, what):
     with pytest.raises(ValueError, match="workspace"):
         rtn.rtn_paged_attention(q, rtn.PagedCache(k, v), table, seq, start, 9, out=torch.empty_like(q),
                                 workspace=WORKSPACES[what](lambda *n, dtype: torch.zeros(*n, dtype=dtype, device=DEV)))
+
+
+# ---- launches ------------------------------------------------------------------------------------------------------------------------
+
+def test_calls_that_no_launch_takes_are_refused():
+    """A launch has fewer than 2^32 threads: more heads, or tiles, are refused before it.  (Nothing here is near to launching: no sizes that fit.)"""
+    cache = lambda D, H: _cache(head_dim=D, kv_heads=H, token_stride=D, head_stride=16 * D, page_stride=16 * D * H)
+    for D in (64, 128, 256):                                   # head_dim / 8 threads a head
+        heads = 2 ** 35 // D // 2 ** 21                        # with 2^21 tokens exactly 2^32 threads
+        assert _rope(tokens=2 ** 21, heads=heads - 16, stride=heads * D, rotary=64, cache=cache(D, 8)) == SHAPE
+        assert _rope(tokens=2 ** 21, heads=heads + 16, stride=(heads + 32) * D, rotary=64, cache=cache(D, 8)) == SHAPE
+    for new in (1, 2 ** 20):
+        assert _attend(tokens=2 ** 20, heads=65536, stride=65536 * 64, cache=cache(64, 1024), B=1, new=new) == SHAPE
+        assert _attend(tokens=2 ** 20, heads=1024, stride=1024 * 64, cache=cache(64, 1024), B=65536, new=new) == SHAPE
+    assert _attend(tokens=2 ** 20 + 1) == SHAPE
+    size = lambda tokens: lib.rtn_paged_attention_workspace_nbytes(tokens, 2, 4, _cache(), 1)
+    assert size(2 ** 20) > 0 and size(2 ** 20 + 1) == 0
