@@ -500,6 +500,11 @@ def _dev_table(t: torch.Tensor):
         raise ValueError("block_table must be an int32 CUDA matrix with contiguous rows")
 
 
+def _c_int(n: int) -> int:
+    """Of a bound that may be any width: what C's int has of it.  (ctypes takes the lower 32 bits.)"""
+    return max(-1, min(n, 2 ** 31 - 1))
+
+
 def _row_stride(t: torch.Tensor) -> int:
     """Elements from row to row; a single row may have any stride."""
     return t.stride(0) if t.shape[0] > 1 else max(t.stride(0), t[0].numel() if t.shape[0] else 0)
@@ -523,6 +528,8 @@ def rtn_cache_plan(step: torch.Tensor, cached_lens: torch.Tensor, block_table: t
     _dev_table(block_table)
     if block_table.shape[0] != B:
         raise ValueError(f"block_table must have a row for each of the {B} requests")
+    if _c_int(page_size) != page_size:
+        raise ValueError("page_size must be 16, 32, 64, 128 or 256")
     if out is None:
         out = CachePlan.empty(B, max_tokens, step.device)
     for t, name, n in zip(out, CachePlan._fields, (B, B + 1, max_tokens, max_tokens, 1, 1)):
@@ -565,7 +572,7 @@ def rtn_rope_cache(qkv: torch.Tensor, q_heads: int, rope: torch.Tensor, position
 
 
 def rtn_paged_attention_workspace_nbytes(tokens: int, requests: int, q_heads: int, cache: PagedCache, max_new: int) -> int:
-    return _lib.rtn_paged_attention_workspace_nbytes(tokens, requests, q_heads, cache._ref, max_new)
+    return _lib.rtn_paged_attention_workspace_nbytes(tokens, requests, q_heads, cache._ref, _c_int(max_new))
 
 
 def rtn_paged_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.Tensor, seq_lens: torch.Tensor, query_start: torch.Tensor, max_new: int,
@@ -578,6 +585,7 @@ def rtn_paged_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.T
         if st is not None:
             _check(st, "rtn_paged_attention")
             return out
+    max_new, window = _c_int(max_new), _c_int(window)
     T, Hq, D = q.shape
     if not (q.is_cuda and q.dtype is cache.dtype and D == cache.head_dim and q.stride(2) == 1 and (q.stride(1) == D or Hq == 1)):
         raise ValueError("q must be a CUDA tensor [tokens, q_heads, head_dim] of the cache's type, contiguous within a token")

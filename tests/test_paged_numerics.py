@@ -4,6 +4,7 @@ the parameter under test.
 u is the unit roundoff of the element type (2^-11 fp16, 2^-8 bf16).  With w_j the softmax weights, an output's error is at most
   u |o| + (1.125 u + e) sum_j w_j |v_j|  (the result's rounding, the weights' rounding, and e, the relative error of a weight: twice the score's)
 plus, in fp16, what weights below its normal range lose.  Scores are sums of D products in fp32: 2 * 2^-23 * (D / 4) * sum |q k| scale."""
+import ctypes as C
 import math
 
 import numpy as np
@@ -221,3 +222,37 @@ def test_calls_that_no_launch_takes_are_refused():
     assert _attend(tokens=2 ** 20 + 1) == SHAPE
     size = lambda tokens: lib.rtn_paged_attention_workspace_nbytes(tokens, 2, 4, _cache(), 1)
     assert size(2 ** 20) > 0 and size(2 ** 20 + 1) == 0
+
+
+# ---- numbers that C's int does not hold ------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("n", [2 ** 31 - 1, 2 ** 31, 2 ** 32 + 4, 2 ** 63 - 1, 2 ** 64 + 5])
+def test_wide_windows_and_bounds_do_not_wrap(launches, n):
+    import paper_2505_15909_amd as rtn
+    q, ints = _on_gpu(2, 4, 128), lambda *n: _on_gpu(*n, dtype=torch.int32)
+    cache, ws = rtn.PagedCache(_on_gpu(4, 2, 16, 128), _on_gpu(4, 2, 16, 128)), _on_gpu(4096, dtype=torch.uint8)
+    rtn.rtn_paged_attention(q, cache, ints(2, 3), ints(2), ints(3), n, window=n, workspace=ws)
+    (_, args), = launches
+    assert C.c_int(args[11]).value == C.c_int(args[14]).value == 2 ** 31 - 1
+    rtn.rtn_paged_attention(q, cache, ints(2, 3), ints(2), ints(3), 1, window=-2 ** 32 + n % 2 ** 32, workspace=ws)
+    assert (C.c_int(launches[1][1][14]).value < 0) == (-2 ** 32 + n % 2 ** 32 < 0)
+    assert rtn.rtn_paged_attention_workspace_nbytes(100, 2, 4, cache, n) == rtn.rtn_paged_attention_workspace_nbytes(100, 2, 4, cache, 100) > 0
+
+
+def test_page_sizes_that_no_int_holds_are_refused(launches):
+    import paper_2505_15909_amd as rtn
+    ints = lambda *n: _on_gpu(*n, dtype=torch.int32)
+    out = rtn.CachePlan(ints(2), ints(3), ints(8), ints(8), ints(1), ints(1))
+    for page_size in (2 ** 32 + 16, -2 ** 32 + 16, 2 ** 64 + 16, -16):
+        with pytest.raises(ValueError, match="page_size"):
+            rtn.rtn_cache_plan(ints(2), ints(2), ints(2, 3), ints(4), ints(1), page_size, 8, out=out)
+    assert not launches
+
+
+@pytest.mark.gpu
+def test_native_attention_leaves_wide_windows_to_be_clipped(rtn):
+    q, k, v, table, seq, start = _attention_case(torch.float16, CAPPED["tiles"], 4, 2, 128, 16)
+    cache = rtn.PagedCache(k, v)
+    ws = torch.empty(rtn.rtn_paged_attention_workspace_nbytes(q.shape[0], 3, 4, cache, 70), dtype=torch.uint8, device=DEV)
+    want = rtn.rtn_paged_attention(q, cache, table, seq, start, 70, workspace=ws).clone()
+    assert torch.equal(rtn.rtn_paged_attention(q, cache, table, seq, start, 70, window=2 ** 32 + 4, workspace=ws, out=torch.empty_like(q)), want)
