@@ -340,7 +340,7 @@ typedef struct {
  *   dev_seq_lens      out  int32 [n_requests]: cached + step, 0 for ended requests
  *   dev_query_start   out  int32 [n_requests + 1]: running sums of the tokens appended
  *   dev_positions, dev_slots   out  int32 [max_tokens]: of new token query_start[b] + i: cached_lens[b] + i, and page * page_size + offset;
- *                     -1 from query_start[n_requests] on
+ *                     -1 from query_start[n_requests] on, and slot -1 for a page that no cache has (negative, or its slots beyond int32)
  *   dev_free_count_out, dev_status   out  int32 [1]
  * status: 0, or everything that does not fit, as a sum of 1 (more pages needed than free_count says and come back), 2 (a row of the table), 4 (max_tokens),
  * 8 (a length or count out of range: cached_lens, free_count, or more pages back, or free after the step, than the stack has entries); the pages and tokens of

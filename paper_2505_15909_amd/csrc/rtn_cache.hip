@@ -149,7 +149,8 @@ __global__ __launch_bounds__(1024) void cache_plan_kernel(const PlanParams p) {
             pos = c + i - start_of(ends, b);
             const int j = pos >> p.shift;
             const int page = j < old ? p.table[b * p.table_stride + j] : popped(start_of(pops, b) + j - old);
-            slot = (int)((uint32_t)page << p.shift) + (pos & (ps - 1));
+            // (a page that no cache can have is no slot, rather than, in 32 bits, one of another page)
+            slot = (uint32_t)page > (uint32_t)INT32_MAX >> p.shift ? -1 : (page << p.shift) + (pos & (ps - 1));
         }
         p.positions[i] = pos;
         p.slots[i] = slot;

@@ -256,3 +256,15 @@ def test_native_attention_leaves_wide_windows_to_be_clipped(rtn):
     ws = torch.empty(rtn.rtn_paged_attention_workspace_nbytes(q.shape[0], 3, 4, cache, 70), dtype=torch.uint8, device=DEV)
     want = rtn.rtn_paged_attention(q, cache, table, seq, start, 70, workspace=ws).clone()
     assert torch.equal(rtn.rtn_paged_attention(q, cache, table, seq, start, 70, window=2 ** 32 + 4, workspace=ws, out=torch.empty_like(q)), want)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("ps", [16, 256])
+@pytest.mark.parametrize("page", [-1, 2 ** 27, 2 ** 28 + 5, 2 ** 31 - 1, -2 ** 31])
+def test_pages_that_no_slot_names_are_not_written(rtn, ps, page):
+    """page * page_size beyond 31 bits is no slot of another page."""
+    ints = lambda *n: torch.tensor(n, dtype=torch.int32, device=DEV)
+    largest = 2 ** 31 // ps - 1                                # its slots are the last that there are
+    plan = rtn.rtn_cache_plan(ints(3, 2, 1), ints(0, ps - 1, 0), ints(-7, -7, page, -7, -7, -7).view(3, 2), ints(9, 9, largest, page, page), ints(5), ps, 6)
+    assert int(plan.status) == 0 and int(plan.free_count) == 2 and plan.positions.tolist() == [0, 1, 2, ps - 1, ps, 0]
+    assert (plan.slots[:5] < 0).all() and int(plan.slots[5]) == largest * ps
