@@ -1,7 +1,7 @@
 // Attention of a batch of requests' new tokens over their pages.
 //
-// A request's queries of one KV head are rows: row r is token r / G and head r % G of the G query heads that share the KV head, so that what is
-// read of K and V serves all of them, in a decode step of one token as in a piece of a prompt.  A workgroup takes a tile of rows of
+// A request's queries of one KV head are rows: row r is token r / G and head r % G of the G query heads that share the KV head, so that what a
+// tile of rows reads of K and V serves all of them, in a decode step of one token as in a piece of a prompt.  A workgroup takes a tile of rows of
 // one request and KV head.  Which request that is it finds from query_start itself: the host knows no lengths.
 //
 // Scores are formed transposed, S^T = K Q^T, one query a lane: the matrix instruction then leaves each lane several keys of one
@@ -45,7 +45,8 @@ __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2
 // softcap tanh(x) log2 e, x = s scale / softcap, for s = q.k, with z = 2 x log2 e = cap_in s.  From |x| = 1/5 on cap_out (1 - 2 / (2^z + 1)), right at both ends, where
 // 2^z is 0 or infinite, with an error of a few ulps of the result.  Below, where that difference would leave an error of cap_out 2^-23 whatever the score, the
 // series of tanh(x) / x (its next term is below 2^-24) times the score without a cap: the error is relative to the score at any cap, one that makes z underflow
-// included.  (Both are formed first, so that the choice is no branch.)
+// included.  (Both are formed first, so that the choice is no branch.  Ten more instructions a score: three prompt pieces on 16 heads of 256 157 us, 146 without the
+// series; a branch for wavefronts without large scores keeps both forms' registers, 166.)
 __device__ __forceinline__ float capped(const AttnParams& p, float s) {
     constexpr double k = 0.12011325347955035;                // x^2 = k z^2
     constexpr float c1 = (float)(-k / 3), c2 = (float)(2 * k * k / 15), c3 = (float)(-17 * k * k * k / 315), limit = 0.57707802f;
@@ -618,8 +619,9 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
         for (int h = 0; h < KT; ++h)
 #pragma unroll
             for (int j = 0; j < 16; ++j) s[h][j] = 0.f;
-        // The operands are read four products ahead, and the wavefront in its products goes before the other workgroup's in its softmax (the two, with
-        // the order of the second product below: 2000 tokens over 30001 2237 -> 2140 us, 4096 tokens of a prompt 183 -> 174).
+        // The operands are read four products ahead (2000 tokens over 30001 1858 us, 1890 without, 1930 without the order of the second product below either; 4096
+        // tokens of a prompt 151, 154, 156), and of a SIMD's two wavefronts the one in its products goes before the one in its softmax (1858 us, 1860 without;
+        // on heads of 256 390 and 392).
         constexpr int kAhead = 4;
         __builtin_amdgcn_s_setprio(1);
         __builtin_amdgcn_sched_barrier(0);
@@ -661,7 +663,8 @@ __device__ __forceinline__ void attend_many(const AttnParams& p, int block_no, u
             for (int j = 0; j < 16; ++j) top = fmaxf(top, s[h][j]);
         top = fmaxf(top, __shfl_xor(top, 32)) * scale;
         // The weights are relative to a maximum that is only followed where it has grown by 2^kLag: they stay below that, exact to the same share, and the
-        // sums, most of the time, need no rescaling.  (fp16 keeps more of its range for small weights.)
+        // sums, most of the time, need no rescaling.  (fp16 keeps more of its range for small weights: 2000 tokens over 30001 1913 us, and
+        // 1911 where it lets 2^8 pass too.)
         constexpr float kLag = TYPE == RTN_TYPE_F16 ? 4.f : 8.f;
         if (__any(top > m + kLag)) {
             const float m_new = fmaxf(m, top), back = m_new == -INFINITY ? 1.f : exp2_of(m - m_new);
@@ -760,7 +763,10 @@ __global__ __launch_bounds__(256, D == 64 && NQ == 1 ? 4 : D == 64 || (D == 128 
     attend_few<TYPE, D, NQ, 4>(p, blockIdx.x, buf, lds[__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)]);
 }
 
-// Requests of few rows and of many in one launch: the tiles' products run beside the others' reading.  Kernels apart for tiles with a cap and without (one for both
+// Requests of few rows and of many in one launch, so that a step of both has no more launches than one of either and its last workgroups are of both kinds.  A compute unit
+// holds one workgroup at a time, of 128 elements by its registers, of 256 by LDS (134.5 KB) as well, so products run beside reading over the chip at most: three
+// pieces of 300 to 900 tokens and 61 decode steps on 32 heads of 128 337 us, 189 and 186 apart; three and 21 on heads of 256 214, 156 and 65.  Heads of 256 take all 256
+// registers and spill 13.  Kernels apart for tiles with a cap and without (one for both
 // keeps the cap's registers where none is: 1024 tokens over 8000 on heads of 256 403 us, 392 so).
 template <int TYPE, int D, bool CAP>
 __global__ __launch_bounds__(512, 2) void attend_mixed_kernel(const AttnParams p) {

@@ -203,7 +203,7 @@ __global__ __launch_bounds__(256) void rope_cache_kernel(const RopeParams p) {
     const T* const src = static_cast<const T*>(p.qkv) + t * p.qkv_stride + (int64_t)h * D;
     const bool rotated = h < p.Hq + p.Hk && c * 8 < p.rotary;
     const int e0 = INTERLEAVED || !rotated ? c * 8 : c * 4, e1 = INTERLEAVED || !rotated ? c * 8 + 4 : p.rotary / 2 + c * 4;
-        const T4 x0 = *reinterpret_cast<const T4*>(src + e0), x1 = *reinterpret_cast<const T4*>(src + e1);
+    const T4 x0 = *reinterpret_cast<const T4*>(src + e0), x1 = *reinterpret_cast<const T4*>(src + e1);
     T4 y0 = x0, y1 = x1;
     const int32_t slot = p.slots[t];
     if (h < p.Hq + p.Hk) {
@@ -280,7 +280,8 @@ extern "C" rtn_status rtn_cache_plan(const int32_t* dev_step, const int32_t* dev
         if (!rtn::aligned_to(q, 4)) return RTN_ERR_ALIGN;
     const rtn::PlanParams p = {dev_step, dev_cached_lens, dev_free_count, dev_block_table, dev_free_pages, dev_seq_lens, dev_query_start, dev_positions,
                                dev_slots, dev_free_count_out, dev_status, table_stride, pool, n_requests, rtn::log2_of(page_size), max_blocks, (int)max_tokens};
-    // In place, one workgroup reads everything before it writes; otherwise a thread has a token or a few.
+    // In place, one workgroup reads everything before it writes; otherwise a thread has a token or a few.  (In the kernel, in place and not: a token each of 64 requests 4.8 and
+    // 4.0 us, of 1024 6.4 and 5.4; 3608 tokens of 64 requests 7.3 and 4.5, 15670 of 1024 19.9 and 5.9.)
     const bool in_place = dev_seq_lens == dev_cached_lens || dev_free_count_out == dev_free_count;
     const int threads = in_place ? 1024 : 256;
     const int64_t work = max_tokens > n_requests ? max_tokens : n_requests;
