@@ -394,6 +394,51 @@ rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int64_t q_stri
                                const int32_t* dev_query_start, int n_requests, int max_new, float scale, float softcap, int window,
                                void* dev_out, void* dev_workspace, size_t workspace_nbytes, void* stream);
 
+/* ---- The 8-bit layer (W8A8).  Weights of 8 bits with a scale for each output channel -- rtn_quantize(bits = 8, group_size <= 0), in the packed
+ * layout that every path reads -- times activations of 8 bits with a scale for each token: sums of whole numbers, at twice the rate of 16-bit ones where
+ * the matrix cores bound a call (prompts), and the same weight stream where memory does.  Between the projections the activations are made by the
+ * three calls of rows below, in the order of a layer: norm -> qkv, quantise -> o, norm -> gate_up, gated activation -> down.
+ *
+ * Quantised rows: codes int8 [rows, dim], row-major and contiguous (8-byte aligned; 16 for the product); scales fp32 [rows].  Of the row's values v (those before any rounding to 16 bits):
+ *   scale = max|v| / 127,  code = rne(v * (127 / max|v|)), -127 .. 127; a row whose largest magnitude is below 2^-100 (for the norm: before
+ *   the row's factor) has scale 0 and codes 0.
+ * 16-bit types: RTN_TYPE_F16, RTN_TYPE_BF16.  Rows of x are x_stride elements apart (a multiple of 8, at least their width), outputs are contiguous;
+ * 0 .. 2^20 rows (0: nothing to do), dim a multiple of 8 up to 65536.  NaN or an infinity in a row gives unspecified results for that row, and for no
+ * other.  Of dev_out (16 bits) and dev_q (codes, with dev_q_scales) exactly one is given.  No output may overlap an input, but for
+ * dev_residual_out, which may be dev_residual or dev_x with the same stride. */
+enum { RTN_ACT_SILU = 0, RTN_ACT_GELU_TANH = 1 };
+
+/* The residual's addition and the root-mean-square norm: h = x + residual, rounded to the type and stored (without a residual h = x and nothing is
+ * stored); v = h * rsqrt(mean(h^2) + eps) * weight.  Sums in fp32: magnitudes from 2^56 (bf16) on overflow them.  eps >= 0; a row of zeros gives zeros.
+ *   dev_residual, dev_residual_out   in, out  [rows, dim], rows their strides apart; both or neither
+ *   dev_weight   in   [dim], in the type */
+rtn_status rtn_norm_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, const void* dev_residual, int64_t residual_stride,
+                         void* dev_residual_out, int64_t residual_out_stride, const void* dev_weight, float eps, void* dev_out, void* dev_q,
+                         float* dev_q_scales, void* stream);
+
+/* The feed-forward's gated activation on the output of a gate-and-up projection: rows of 2 dim elements, a the first dim, b the others:
+ *   v = act(a) * b,  act(a) = a / (1 + exp(-a)) (RTN_ACT_SILU) or a / 2 (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) (RTN_ACT_GELU_TANH), in fp32. */
+rtn_status rtn_gated_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, int activation, void* dev_out, void* dev_q,
+                          float* dev_q_scales, void* stream);
+
+/* v = x. */
+rtn_status rtn_quantize_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, void* dev_q, float* dev_q_scales, void* stream);
+
+/* out[m, k] = code[m, k] * scale[m], rounded once to the type: for a module that takes 16 bits beside one that takes 8. */
+rtn_status rtn_dequantize_rows(const void* dev_q, const float* dev_q_scales, int64_t rows, int64_t dim, int dtype, void* dev_out, void* stream);
+
+/* C[m, n] = T( (sum_k q[m, k] * w[n, k]) * (q_scale[m] * scale[n]) ), the sum exact in 32-bit integers, the rest in fp32, rounded once.
+ *   dev_q          in   int8 [M, K] row-major (any codes, -128 included); dev_q_scales fp32 [M]
+ *   dev_qweight    in   packed 8-bit codes [N, K] of rtn_quantize with one group a row; dev_scales fp16 [N]
+ *   dev_C          out  [M, N] in `dtype`, RTN_TYPE_F16 or RTN_TYPE_BF16
+ *   dev_workspace  scratch for the partial sums of K splits, rtn_linear_w8a8_workspace_nbytes() bytes (at most 64 MiB); with less or NULL K is split less
+ *                  (slower, not an error); contents undefined before and after; calls that overlap in time need distinct ones
+ * N % 16 == 0, K % 256 == 0, K < 2^17 (so that no sum leaves 32 bits), N * K below 0x7FFF0000, M 0 .. 2^20 (0: nothing to do), N <= 2^30.  The sums being exact, a
+ * call gives the same bits whatever its workspace. */
+size_t rtn_linear_w8a8_workspace_nbytes(int64_t M, int64_t N, int64_t K);
+rtn_status rtn_linear_w8a8(const void* dev_q, const float* dev_q_scales, int64_t M, const void* dev_qweight, const void* dev_scales, int64_t N, int64_t K,
+                           int dtype, void* dev_C, void* dev_workspace, size_t workspace_nbytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -111,6 +111,18 @@ def _load() -> C.CDLL:
     lib.rtn_paged_attention.restype = ci
     lib.rtn_paged_attention.argtypes = [vp, i64, i64, ci, C.POINTER(rtn_kv_cache), vp, i64, ci, vp, vp, ci, ci, C.c_float, C.c_float, ci,
                                         vp, vp, sz, vp]
+    lib.rtn_norm_rows.restype = ci
+    lib.rtn_norm_rows.argtypes = [vp, i64, i64, i64, ci, vp, i64, vp, i64, vp, C.c_float, vp, vp, vp, vp]
+    lib.rtn_gated_rows.restype = ci
+    lib.rtn_gated_rows.argtypes = [vp, i64, i64, i64, ci, ci, vp, vp, vp, vp]
+    lib.rtn_quantize_rows.restype = ci
+    lib.rtn_quantize_rows.argtypes = [vp, i64, i64, i64, ci, vp, vp, vp]
+    lib.rtn_dequantize_rows.restype = ci
+    lib.rtn_dequantize_rows.argtypes = [vp, vp, i64, i64, ci, vp, vp]
+    lib.rtn_linear_w8a8_workspace_nbytes.restype = sz
+    lib.rtn_linear_w8a8_workspace_nbytes.argtypes = [i64, i64, i64]
+    lib.rtn_linear_w8a8.restype = ci
+    lib.rtn_linear_w8a8.argtypes = [vp, vp, i64, vp, vp, i64, i64, ci, vp, vp, sz, vp]
     return lib
 
 
@@ -142,7 +154,8 @@ EXPORTS = ["rtn_status_str", "rtn_layout_version", "rtn_qweight_nbytes", "rtn_sc
            "rtn_problem_status", "rtn_linear_validate", "rtn_linear_noalloc", "rtn_unpack", "rtn_dequantize", "rtn_gemm_fp16", "rtn_dense_weight_nbytes", "rtn_linear_dense",
            "rtn_quantize_asym", "rtn_dequantize_asym", "rtn_linear_asym",
            "rtn_layer_forward", "rtn_grouped_forward", "rtn_bench_read_stream", "rtn_plan_bits", "rtn_plan_effective_bits",
-           "rtn_cache_plan", "rtn_rope_cache", "rtn_paged_attention_workspace_nbytes", "rtn_paged_attention"]
+           "rtn_cache_plan", "rtn_rope_cache", "rtn_paged_attention_workspace_nbytes", "rtn_paged_attention",
+           "rtn_norm_rows", "rtn_gated_rows", "rtn_quantize_rows", "rtn_dequantize_rows", "rtn_linear_w8a8_workspace_nbytes", "rtn_linear_w8a8"]
 
 
 def _check(status: int, what: str):
@@ -606,4 +619,136 @@ def rtn_paged_attention(q: torch.Tensor, cache: PagedCache, block_table: torch.T
     _check(_lib.rtn_paged_attention(q.data_ptr(), T, _row_stride(q), Hq, cache._ref, block_table.data_ptr(), _row_stride(block_table), block_table.shape[1],
                                     seq_lens.data_ptr(), query_start.data_ptr(), B, max_new, D ** -0.5 if scale is None else scale, softcap, window,
                                     out.data_ptr(), workspace.data_ptr(), workspace.nbytes, _stream()), "rtn_paged_attention")
+    return out
+
+
+# ---- The 8-bit layer: rows of activations in 8 bits with a scale for each token, and their product with 8-bit weights --------------------
+
+RTN_ACT_SILU, RTN_ACT_GELU_TANH = 0, 1
+ACTIVATION = {"silu": RTN_ACT_SILU, "gelu_tanh": RTN_ACT_GELU_TANH}
+
+
+def _dev_current(t: torch.Tensor, name: str):
+    """Kernels are launched on the current device's stream: memory of another one is not for them."""
+    if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        raise ValueError(f"{name} must be on the current CUDA device")
+
+
+def _dev_rows(t: torch.Tensor, name: str, shape=None, dtype=None):
+    """A 16-bit matrix with contiguous rows, any distance apart."""
+    _dev_current(t, name)
+    if not (t.dim() == 2 and t.dtype in _TYPES and (dtype is None or t.dtype is dtype) and (shape is None or t.shape == shape) and
+            (t.stride(1) == 1 or t.shape[1] == 1)):
+        raise ValueError(f"{name} must be an fp16 or bf16 matrix with contiguous rows" + ("" if shape is None else f", {list(shape)} of x's type"))
+
+
+def _dev_whole(t: torch.Tensor, name: str, shape, dtype):
+    _dev_current(t, name)
+    if not (t.dtype is dtype and t.shape == shape and t.is_contiguous()):
+        raise ValueError(f"{name} must be contiguous, {list(shape)} of {dtype}")
+
+
+def _apart(t: torch.Tensor) -> int:
+    """Elements from row to row of a matrix; of a single row, or none, the stride says nothing."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+def _row_outputs(rows: int, dim: int, dtype, quantize: bool, out, device):
+    """What a call of rows writes: 16 bits, or codes and scales, made or as given; and the three pointers of the C entry."""
+    if not quantize:
+        if out is None:
+            out = torch.empty((rows, dim), dtype=dtype, device=device)
+        _dev_whole(out, "out", (rows, dim), dtype)
+        return out, (out.data_ptr(), None, None)
+    if out is None:
+        out = torch.empty((rows, dim), dtype=torch.int8, device=device), torch.empty(rows, dtype=torch.float32, device=device)
+    q, scales = out
+    _dev_whole(q, "out[0]", (rows, dim), torch.int8)
+    _dev_whole(scales, "out[1]", (rows,), torch.float32)
+    return (q, scales), (None, q.data_ptr(), scales.data_ptr())
+
+
+def rtn_norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor = None, eps: float = 1e-6, quantize: bool = False,
+                  residual_out: torch.Tensor = None, out=None):
+    """x [rows, dim] (+ residual, the sum of which goes to residual_out, or back to residual) -> its root-mean-square norm times weight, in x's type,
+    or quantised: (int8 [rows, dim], fp32 scales [rows])."""
+    _dev_rows(x, "x")
+    M, K = x.shape
+    _dev_whole(weight, "weight", (K,), x.dtype)
+    if residual is None:
+        if residual_out is not None:
+            raise ValueError("residual_out is given without a residual")
+        add = (None, 0, None, 0)
+    else:
+        residual_out = residual if residual_out is None else residual_out
+        _dev_rows(residual, "residual", x.shape, x.dtype)
+        _dev_rows(residual_out, "residual_out", x.shape, x.dtype)
+        add = (residual.data_ptr(), _apart(residual), residual_out.data_ptr(), _apart(residual_out))
+    out, to = _row_outputs(M, K, x.dtype, quantize, out, x.device)
+    _check(_lib.rtn_norm_rows(x.data_ptr(), M, _apart(x), K, _TYPES[x.dtype], *add, weight.data_ptr(), eps, *to, _stream()), "rtn_norm_rows")
+    return out
+
+
+def rtn_gated_rows(x: torch.Tensor, activation: str = "silu", quantize: bool = False, out=None):
+    """x [rows, 2 dim], gate and up side by side as their projection gives them -> act(gate) * up in x's type, or quantised as rtn_norm_rows gives it.
+    activation: "silu" or "gelu_tanh"."""
+    _dev_rows(x, "x")
+    M, K = x.shape[0], x.shape[1] // 2
+    if x.shape[1] != 2 * K:
+        raise ValueError("x must have an even number of columns")
+    if activation not in ACTIVATION:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATION)}")
+    out, to = _row_outputs(M, K, x.dtype, quantize, out, x.device)
+    _check(_lib.rtn_gated_rows(x.data_ptr(), M, _apart(x), K, _TYPES[x.dtype], ACTIVATION[activation], *to, _stream()), "rtn_gated_rows")
+    return out
+
+
+def rtn_quantize_rows(x: torch.Tensor, out=None):
+    """x [rows, dim] -> (int8 [rows, dim], fp32 scales [rows])."""
+    _dev_rows(x, "x")
+    M, K = x.shape
+    out, to = _row_outputs(M, K, x.dtype, True, out, x.device)
+    _check(_lib.rtn_quantize_rows(x.data_ptr(), M, _apart(x), K, _TYPES[x.dtype], *to[1:], _stream()), "rtn_quantize_rows")
+    return out
+
+
+def rtn_dequantize_rows(q: torch.Tensor, q_scales: torch.Tensor, dtype: torch.dtype = torch.float16, out: torch.Tensor = None) -> torch.Tensor:
+    """The values that quantised rows stand for, in `dtype` (or out's)."""
+    dtype = dtype if out is None else out.dtype
+    if q.dim() != 2 or dtype not in _TYPES:
+        raise ValueError("q must be a matrix, and its values fp16 or bf16")
+    M, K = q.shape
+    _dev_whole(q, "q", (M, K), torch.int8)
+    _dev_whole(q_scales, "q_scales", (M,), torch.float32)
+    if out is None:
+        out = torch.empty((M, K), dtype=dtype, device=q.device)
+    _dev_whole(out, "out", (M, K), dtype)
+    _check(_lib.rtn_dequantize_rows(q.data_ptr(), q_scales.data_ptr(), M, K, _TYPES[dtype], out.data_ptr(), _stream()), "rtn_dequantize_rows")
+    return out
+
+
+def rtn_linear_w8a8_workspace_nbytes(M: int, N: int, K: int) -> int:
+    return _lib.rtn_linear_w8a8_workspace_nbytes(M, N, K)
+
+
+def rtn_linear_w8a8(q: torch.Tensor, q_scales: torch.Tensor, qweight: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.float16,
+                    out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
+    """Quantised rows int8 [M, K] with fp32 scales [M] times rtn_quantize(W, 8, 0)'s qweight and fp16 scales [N, 1] -> [M, N] in `dtype` (or out's)."""
+    dtype = dtype if out is None else out.dtype
+    if q.dim() != 2 or dtype not in _TYPES:
+        raise ValueError("q must be a matrix, and the result fp16 or bf16")
+    M, K = q.shape
+    N = scales.shape[0] if scales.dim() else 0
+    _dev_whole(q, "q", (M, K), torch.int8)
+    _dev_whole(q_scales, "q_scales", (M,), torch.float32)
+    _dev_whole(scales, "scales", (N, 1), torch.float16)
+    _dev_whole(qweight, "qweight", (N * K,), torch.uint8)
+    if out is None:
+        out = torch.empty((M, N), dtype=dtype, device=q.device)
+    _dev_whole(out, "out", (M, N), dtype)
+    if workspace is None:
+        workspace = torch.empty(max(16, _lib.rtn_linear_w8a8_workspace_nbytes(M, N, K)), dtype=torch.uint8, device=q.device)
+    _dev_workspace(workspace, q.device)
+    _check(_lib.rtn_linear_w8a8(q.data_ptr(), q_scales.data_ptr(), M, qweight.data_ptr(), scales.data_ptr(), N, K, _TYPES[dtype], out.data_ptr(),
+                                workspace.data_ptr(), workspace.nbytes, _stream()), "rtn_linear_w8a8")
     return out

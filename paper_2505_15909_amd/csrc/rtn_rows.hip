@@ -1,0 +1,269 @@
+// Rows of activations in 8 bits: the residual's addition with the root-mean-square norm, the feed-forward's gated activation, and plain
+// rows, quantised with a scale for each token (or, the first two, left in 16 bits).
+//
+// Every one of them is v_k times a factor of the row: v = h w with the factor rsqrt(mean(h^2) + eps) for the norm, v = act(a) b and v = x
+// with 1.  The largest |v| and the sum of squares are found in one sweep and the codes are rne(v * 127 / max|v|), which the factor does not
+// enter; so a row is read once, kept in registers, and meets once over the workgroup, not once for the norm and again for the scale.
+// h w is exact in fp32 (two significands of at most 11 bits), so a code is the exact product's rounding by one reciprocal of 24 bits.
+//
+// Bound by memory: the norm with a residual moves 7 bytes an element quantised, the gated activation 5, plain rows 3.
+#include "rtn_paged.h"
+
+namespace rtn {
+
+enum { ROW_PLAIN = 0, ROW_NORM = 1, ROW_GATED = 2 };
+
+struct RowParams {
+    const void *x, *residual, *weight;
+    void *sum, *out;
+    float* scales;
+    int64_t x_stride, residual_stride, sum_stride;
+    int rows, dim, gelu;
+    float eps, inv_dim;
+};
+
+constexpr float kLeastRow = 0x1p-100f;                       // rows whose largest magnitude is below have scale 0 and codes 0
+
+// Of values that are not negative, in every lane; NaN stays.
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+__device__ __forceinline__ float wave_total(float x) {
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, wave_scan(x)), 63));
+}
+
+__device__ __forceinline__ float wave_largest(float x) {
+    x = larger(x, from_lane<0x111, 0xF>(x));
+    x = larger(x, from_lane<0x112, 0xF>(x));
+    x = larger(x, from_lane<0x114, 0xF>(x));
+    x = larger(x, from_lane<0x118, 0xF>(x));
+    x = larger(x, from_lane<0x142, 0xA>(x));
+    x = larger(x, from_lane<0x143, 0xC>(x));
+    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// act(a) b.  Both activations are a / (1 + exp(-z)): z = a, or a sqrt(8 / pi) (1 + 0.044715 a^2), for which it is a / 2 (1 + tanh(z / 2)).
+__device__ __forceinline__ float gated(float a, float b, bool gelu) {
+    const float z = gelu ? a * fmaf(a * a, 0.071354816f, 1.5957691f) : a;
+    return a * __builtin_amdgcn_rcpf(1.0f + expf(-z)) * b;
+}
+
+// Four codes of values within +-127: adding 1.5 2^23 rounds to nearest even and leaves the code in the lowest byte.
+__device__ __forceinline__ uint32_t four_codes(const float* v, float inv) {
+    uint32_t t[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) t[i] = __builtin_bit_cast(uint32_t, fmaf(v[i], inv, 12582912.0f));
+    return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], 0x0C0C0400u), __builtin_amdgcn_perm(t[1], t[0], 0x0C0C0400u), 0x05040100u);
+}
+
+// T threads a row, C pieces of eight elements a thread; workgroups of at least 256 threads.
+template <int TYPE, int OP, bool QUANT, int T, int C>
+__global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams p) {
+    typedef typename Elem<TYPE>::one E;
+    typedef typename Elem<TYPE>::x8 E8;
+    constexpr int ROWS = T < 256 ? 256 / T : 1, WAVES = T / 64;
+    __shared__ float part[2][WAVES];
+    const int t = threadIdx.x % T, row = (int)blockIdx.x * ROWS + (int)threadIdx.x / T;
+    if (row >= p.rows) return;                               // (a whole wavefront; with more wavefronts a row there is one row)
+    const E* const x = static_cast<const E*>(p.x) + row * p.x_stride;
+    // Everything is requested before the first store (which may be to the same memory).  What is kept for the second sweep: the elements, the
+    // norm's with its weight; of the gated activation the values, whose exponentials are not formed twice.
+    E8 in[C], with[C], weight[OP == ROW_NORM ? C : 1];
+    float kept[OP == ROW_GATED ? C : 1][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int k = (c * T + t) * 8;
+        if (k >= p.dim) continue;
+        in[c] = *reinterpret_cast<const E8*>(x + k);
+        if constexpr (OP == ROW_GATED) with[c] = *reinterpret_cast<const E8*>(x + p.dim + k);
+        if constexpr (OP == ROW_NORM) {
+            if (p.residual) with[c] = *reinterpret_cast<const E8*>(static_cast<const E*>(p.residual) + row * p.residual_stride + k);
+            weight[c] = *reinterpret_cast<const E8*>(static_cast<const E*>(p.weight) + k);
+        }
+    }
+    auto value = [&](int c, int i) -> float {
+        if constexpr (OP == ROW_GATED) return kept[c][i];
+        else if constexpr (OP == ROW_NORM) return (float)in[c][i] * (float)weight[c][i];
+        else return (float)in[c][i];
+    };
+    float square = 0.f, most = 0.f;
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int k = (c * T + t) * 8;
+        if (k >= p.dim) continue;
+        if constexpr (OP == ROW_NORM)
+            if (p.residual) {
+                // the sum is held in the type, as the next layer finds it, and what is held is normed
+#pragma unroll
+                for (int i = 0; i < 8; ++i) in[c][i] = (E)((float)in[c][i] + (float)with[c][i]);
+                *reinterpret_cast<E8*>(static_cast<E*>(p.sum) + row * p.sum_stride + k) = in[c];
+            }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float a = (float)in[c][i];
+            if constexpr (OP == ROW_NORM) square = fmaf(a, a, square);
+            if constexpr (OP == ROW_GATED) kept[c][i] = gated(a, (float)with[c][i], p.gelu);
+            if constexpr (QUANT) most = larger(most, fabsf(value(c, i)));
+        }
+    }
+    if constexpr (OP == ROW_NORM) square = wave_total(square);
+    if constexpr (QUANT) most = wave_largest(most);
+    if constexpr (WAVES > 1 && (QUANT || OP == ROW_NORM)) {
+        if (t % 64 == 0) {
+            part[0][t / 64] = square;
+            part[1][t / 64] = most;
+        }
+        __syncthreads();
+        square = part[0][0];
+        most = part[1][0];
+#pragma unroll
+        for (int w = 1; w < WAVES; ++w) {
+            square += part[0][w];
+            most = larger(most, part[1][w]);
+        }
+    }
+    float factor = 1.f;
+    if constexpr (OP == ROW_NORM) {
+        const float mean = fmaf(square, p.inv_dim, p.eps);
+        factor = mean == 0.f ? 0.f : rsqrtf(mean);           // (a row of zeros without eps)
+    }
+    float inv = 0.f;
+    if constexpr (QUANT) {
+        const bool none = most < kLeastRow;
+        inv = none ? 0.f : 127.0f / most;
+        if (t == 0) p.scales[row] = none ? 0.f : most * factor / 127.0f;
+    }
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+        const int k = (c * T + t) * 8;
+        if (k >= p.dim) continue;
+        if constexpr (QUANT) {
+            float v[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = value(c, i);
+            const u32x2_t codes = {four_codes(v, inv), four_codes(v + 4, inv)};
+            *reinterpret_cast<u32x2_t*>(static_cast<uint8_t*>(p.out) + (int64_t)row * p.dim + k) = codes;
+        } else {
+            E8 y;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) y[i] = (E)(value(c, i) * factor);
+            *reinterpret_cast<E8*>(static_cast<E*>(p.out) + (int64_t)row * p.dim + k) = y;
+        }
+    }
+}
+
+// A thread has up to four pieces of eight codes of a row; segments of 8192 elements.
+template <int TYPE>
+__global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint8_t* q, const float* scales, void* out, int dim, int segments) {
+    typedef typename Elem<TYPE>::one E;
+    typedef typename Elem<TYPE>::x8 E8;
+    const int row = blockIdx.x / segments, segment = blockIdx.x - row * segments;
+    const float s = scales[row];
+    const int64_t at = (int64_t)row * dim;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+        const int k = segment * 8192 + (c * 256 + (int)threadIdx.x) * 8;
+        if (k >= dim) return;
+        const u32x2_t codes = *reinterpret_cast<const u32x2_t*>(q + at + k);
+        E8 y;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) y[i] = (E)((float)(int8_t)(codes[i / 4] >> (i % 4 * 8)) * s);
+        *reinterpret_cast<E8*>(static_cast<E*>(out) + at + k) = y;
+    }
+}
+
+template <int TYPE, int OP, bool QUANT, int T, int C>
+static void launch_rows_as(const RowParams& p, hipStream_t st) {
+    constexpr int ROWS = T < 256 ? 256 / T : 1;
+    hipLaunchKernelGGL((rows_kernel<TYPE, OP, QUANT, T, C>), dim3((unsigned)((p.rows + ROWS - 1) / ROWS)), dim3(T < 256 ? 256 : T), 0, st, p);
+}
+
+template <int TYPE, int OP, bool QUANT>
+static hipError_t launch_rows(const RowParams& p, hipStream_t st) {
+    const int pieces = p.dim / 8;
+    if (pieces <= 64) launch_rows_as<TYPE, OP, QUANT, 64, 1>(p, st);
+    else if (pieces <= 256) launch_rows_as<TYPE, OP, QUANT, 256, 1>(p, st);
+    else if (pieces <= 512) launch_rows_as<TYPE, OP, QUANT, 256, 2>(p, st);
+    else if (pieces <= 1024) launch_rows_as<TYPE, OP, QUANT, 256, 4>(p, st);
+    else if (pieces <= 2048) launch_rows_as<TYPE, OP, QUANT, 1024, 2>(p, st);
+    else if (pieces <= 4096) launch_rows_as<TYPE, OP, QUANT, 1024, 4>(p, st);
+    else launch_rows_as<TYPE, OP, QUANT, 1024, 8>(p, st);
+    return hipGetLastError();
+}
+
+template <int OP, bool QUANT>
+static rtn_status launch_typed(const RowParams& p, int dtype, void* stream) {
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    return (dtype == RTN_TYPE_F16 ? launch_rows<RTN_TYPE_F16, OP, QUANT>(p, st) : launch_rows<RTN_TYPE_BF16, OP, QUANT>(p, st)) == hipSuccess ? RTN_OK : RTN_ERR_HIP;
+}
+
+static bool row_sizes_fit(int64_t rows, int64_t dim) { return rows >= 0 && rows <= 1 << 20 && dim >= 8 && dim <= 65536 && dim % 8 == 0; }
+
+// Rows of `width` elements, `stride` apart: the status that they alone give.
+static rtn_status check_rows(const void* p, int64_t stride, int64_t width) {
+    if (stride < width || stride > (int64_t)1 << 36) return RTN_ERR_SHAPE;
+    return stride % 8 || !aligned_to(p, 16) ? RTN_ERR_ALIGN : RTN_OK;
+}
+
+// What every entry checks of its output: one of 16 bits, or codes and scales.
+static rtn_status check_outputs(int64_t rows, int64_t dim, int dtype, const void* out16, const void* codes, const void* scales) {
+    if (rows != 0 && (!out16 == !codes || (codes && !scales))) return RTN_ERR_NULL;
+    if (dtype != RTN_TYPE_F16 && dtype != RTN_TYPE_BF16) return RTN_ERR_CONFIG;
+    if (!row_sizes_fit(rows, dim)) return RTN_ERR_SHAPE;
+    return aligned_to(out16, 16) && aligned_to(codes, 8) && aligned_to(scales, 4) ? RTN_OK : RTN_ERR_ALIGN;
+}
+
+}  // namespace rtn
+
+extern "C" rtn_status rtn_norm_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, const void* dev_residual, int64_t residual_stride,
+                                    void* dev_residual_out, int64_t residual_out_stride, const void* dev_weight, float eps, void* dev_out, void* dev_q,
+                                    float* dev_q_scales, void* stream) {
+    if (rows != 0 && (!dev_x || !dev_weight || !dev_residual != !dev_residual_out)) return RTN_ERR_NULL;
+    rtn_status st = rtn::check_outputs(rows, dim, dtype, dev_out, dev_q, dev_q_scales);
+    if (st == RTN_OK) st = rtn::check_rows(dev_x, x_stride, dim);
+    if (st == RTN_OK && dev_residual) st = rtn::check_rows(dev_residual, residual_stride, dim);
+    if (st == RTN_OK && dev_residual) st = rtn::check_rows(dev_residual_out, residual_out_stride, dim);
+    if (st != RTN_OK) return st;
+    if (!rtn::aligned_to(dev_weight, 16)) return RTN_ERR_ALIGN;
+    if (!(eps >= 0.f)) return RTN_ERR_CONFIG;
+    if (rows == 0) return RTN_OK;
+    const rtn::RowParams p = {dev_x, dev_residual, dev_weight, dev_residual_out, dev_q ? dev_q : dev_out, dev_q_scales, x_stride, residual_stride,
+                              residual_out_stride, (int)rows, (int)dim, 0, eps, 1.0f / (float)dim};
+    return dev_q ? rtn::launch_typed<rtn::ROW_NORM, true>(p, dtype, stream) : rtn::launch_typed<rtn::ROW_NORM, false>(p, dtype, stream);
+}
+
+extern "C" rtn_status rtn_gated_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, int activation, void* dev_out, void* dev_q,
+                                     float* dev_q_scales, void* stream) {
+    if (rows != 0 && !dev_x) return RTN_ERR_NULL;
+    rtn_status st = rtn::check_outputs(rows, dim, dtype, dev_out, dev_q, dev_q_scales);
+    if (st == RTN_OK) st = rtn::check_rows(dev_x, x_stride, 2 * dim);
+    if (st != RTN_OK) return st;
+    if (activation != RTN_ACT_SILU && activation != RTN_ACT_GELU_TANH) return RTN_ERR_CONFIG;
+    if (rows == 0) return RTN_OK;
+    const rtn::RowParams p = {dev_x, nullptr, nullptr, nullptr, dev_q ? dev_q : dev_out, dev_q_scales, x_stride, 0, 0, (int)rows, (int)dim,
+                              activation == RTN_ACT_GELU_TANH, 0.f, 0.f};
+    return dev_q ? rtn::launch_typed<rtn::ROW_GATED, true>(p, dtype, stream) : rtn::launch_typed<rtn::ROW_GATED, false>(p, dtype, stream);
+}
+
+extern "C" rtn_status rtn_quantize_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, void* dev_q, float* dev_q_scales, void* stream) {
+    if (rows != 0 && !dev_x) return RTN_ERR_NULL;
+    rtn_status st = rtn::check_outputs(rows, dim, dtype, nullptr, dev_q, dev_q_scales);
+    if (st == RTN_OK) st = rtn::check_rows(dev_x, x_stride, dim);
+    if (st != RTN_OK || rows == 0) return st;
+    const rtn::RowParams p = {dev_x, nullptr, nullptr, nullptr, dev_q, dev_q_scales, x_stride, 0, 0, (int)rows, (int)dim, 0, 0.f, 0.f};
+    return rtn::launch_typed<rtn::ROW_PLAIN, true>(p, dtype, stream);
+}
+
+extern "C" rtn_status rtn_dequantize_rows(const void* dev_q, const float* dev_q_scales, int64_t rows, int64_t dim, int dtype, void* dev_out, void* stream) {
+    if (rows != 0 && (!dev_q || !dev_q_scales || !dev_out)) return RTN_ERR_NULL;
+    if (dtype != RTN_TYPE_F16 && dtype != RTN_TYPE_BF16) return RTN_ERR_CONFIG;
+    if (!rtn::row_sizes_fit(rows, dim)) return RTN_ERR_SHAPE;
+    if (!rtn::aligned_to(dev_q, 8) || !rtn::aligned_to(dev_out, 16) || !rtn::aligned_to(dev_q_scales, 4)) return RTN_ERR_ALIGN;
+    if (rows == 0) return RTN_OK;
+    const int segments = (int)((dim + 8191) / 8192);
+    const dim3 grid((unsigned)(rows * segments));
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const uint8_t* q = static_cast<const uint8_t*>(dev_q);
+    if (dtype == RTN_TYPE_F16) hipLaunchKernelGGL((rtn::dequantize_rows_kernel<RTN_TYPE_F16>), grid, dim3(256), 0, st, q, dev_q_scales, dev_out, (int)dim, segments);
+    else hipLaunchKernelGGL((rtn::dequantize_rows_kernel<RTN_TYPE_BF16>), grid, dim3(256), 0, st, q, dev_q_scales, dev_out, (int)dim, segments);
+    return hipGetLastError() == hipSuccess ? RTN_OK : RTN_ERR_HIP;
+}
