@@ -20,10 +20,9 @@ __device__ __forceinline__ int4_t weight_operand(u32x4_t c) {
 }
 
 template <int TYPE>
-__device__ __forceinline__ u32x2_t four_results(int4_t sum, float row_scale, const half_t* scales) {
+__device__ __forceinline__ u32x2_t four_results(int4_t sum, float row_scale, half4_t s) {
     typedef typename Elem<TYPE>::x4 E4;
     typedef typename Elem<TYPE>::one E;
-    const half4_t s = *reinterpret_cast<const half4_t*>(scales);
     E4 y;
 #pragma unroll
     for (int e = 0; e < 4; ++e) y[e] = (E)((float)sum[e] * (row_scale * (float)s[e]));
@@ -125,7 +124,220 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
         if (m >= p.M || c >= p.N) continue;
         const int64_t at = (int64_t)m * p.N + c;
         if (p.split > 1) *reinterpret_cast<int4_t*>(p.ws + (int64_t)z * p.M * p.N + at) = s;
-        else *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, p.a_scales[m], p.scales + c);
+        else *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, p.a_scales[m], *reinterpret_cast<const half4_t*>(p.scales + c));
+    }
+}
+
+// ---- Many rows: bound by the matrix cores, at the clock that the power allows.  A workgroup of 8 wavefronts (2 along M x 4 along N) computes
+// 32 MBW rows x 256 columns of C, a wavefront 16 MBW x 64 of them.  K advances by 128 columns a step: 128 bytes of a row are eight 16-byte pieces in
+// LDS, piece p at slot p ^ (row & 7) (conflict-free both ways); packed tiles lie as they are, a lane reads its own chunk.  Both come
+// straight into LDS, SA and SB steps ahead.  A step runs in phases of two row blocks and both halves of its columns; a phase reads the next one's operands, and
+// the one barrier of a step stands before its last phase, whose operands are in registers by then: the stage is free behind it, and the
+// requests for it go out over the phases that follow. ----
+constexpr int kTileN = 256, kTileThreads = 512;
+constexpr int kBufferFlags = 0x00020000;
+constexpr uint32_t kNoRow = 0x80000000u;                     // beyond every resource: reads zeros
+constexpr int kZGroup = 4;
+
+// 16 bytes per lane from global memory into 1 KiB of LDS at a wave-uniform address
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint8_t* lds, uint32_t lane_off, int off) {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void*)lds, 16, lane_off, off, 0, 0);
+}
+
+// Workgroup barrier behind the loads older than the N newest ones and every LDS access.
+template <int N>
+__device__ __forceinline__ void wait_and_barrier() {
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" :: "n"(N) : "memory");
+}
+
+template <int TYPE, int MBW>
+__global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Params p) {
+    constexpr int TM = 32 * MBW, A_BYTES = TM * 128, B_BYTES = kTileN * 128;
+    constexpr int PH = MBW / 2;                              // phases of a step
+    constexpr int SA = MBW == 4 ? 3 : 2, SB = 3;             // stages: 144 or 160 KiB
+    constexpr int AP = 2, BP = PH == 4 ? 2 : 0;              // the activations' requests go out in AP phases from the barrier on, the weights' from phase BP on
+    constexpr int NA = TM / 64, NB = kTileN / 64;            // requests of a wavefront and step, 1 KiB each
+    constexpr int U = 6;                                     // steps a turn of the loop: every stage index is a literal
+    __shared__ __align__(16) uint8_t lds_a0[A_BYTES], lds_a1[A_BYTES], lds_a2[SA > 2 ? A_BYTES : 16];
+    __shared__ __align__(16) uint8_t lds_b0[B_BYTES], lds_b1[B_BYTES], lds_b2[B_BYTES];
+    auto stage_a = [&](int i) { return i == 0 ? lds_a0 : i == 1 ? lds_a1 : lds_a2; };
+    auto stage_b = [&](int i) { return i == 0 ? lds_b0 : i == 1 ? lds_b1 : lds_b2; };
+
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave >> 2, wn = wave & 3, nl = lane & 15, kq = lane >> 4;
+    const int blocks = (p.XB * p.YB + kXcds - 1) / kXcds * kXcds, z = blockIdx.x / blocks;
+    int xb, yb;
+    if (!xcd_tile((int)blockIdx.x - z * blocks, p.XB, p.YB, kZGroup, &xb, &yb)) return;
+    const int m0 = yb * TM, n0 = xb * kTileN, K = p.KT * 64;
+    const int pairs = p.KT / 4;                              // (two steps each: a workgroup has an even number of them)
+    const int s0 = 2 * (int)((int64_t)pairs * z / p.split), T = 2 * (int)((int64_t)pairs * (z + 1) / p.split) - s0;
+
+    // Both operands through resources that start at this workgroup's first row; rows past M or N read zeros, steps past the last one the last.
+    const int a_rows = min(TM, p.M - m0), b_tiles = min(kTileN, p.N - n0) / 16;
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.A) + (int64_t)m0 * K, 0, (uint32_t)a_rows * (uint32_t)K, kBufferFlags);
+    const __amdgpu_buffer_rsrc_t rb =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.B) + (int64_t)(n0 / 16) * p.KT * 1024, 0, (uint32_t)b_tiles * (uint32_t)p.KT * 1024u, kBufferFlags);
+    uint32_t a_lane[NA], b_lane[NB / 2];
+    const int st_row = lane >> 3, st_piece = (lane & 7) ^ (lane >> 3);
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+        const int row = (wave * NA + i) * 8 + st_row;
+        a_lane[i] = row < a_rows ? (uint32_t)row * (uint32_t)K + st_piece * 16 : kNoRow;
+    }
+#pragma unroll
+    for (int i = 0; i < NB / 2; ++i) {
+        const int row = wave * (NB / 2) + i;
+        b_lane[i] = row < b_tiles ? (uint32_t)row * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
+    }
+    auto a_dma = [&](int stage, int t, int i) { load_to_lds(ra, stage_a(stage) + (wave * NA + i) * 1024, a_lane[i], (s0 + min(t, T - 1)) * 128); };
+    auto b_dma = [&](int stage, int t, int i) {
+        load_to_lds(rb, stage_b(stage) + (wave * NB + i) * 1024, b_lane[i >> 1], (s0 + min(t, T - 1)) * 2048 + (i & 1) * 1024);
+    };
+
+    int4_t acc[MBW][4];
+#pragma unroll
+    for (int b = 0; b < MBW; ++b)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) acc[b][r] = (int4_t){0, 0, 0, 0};
+    const uint32_t a_rd = (uint32_t)((wm * (TM / 2) + nl) * 128), b_rd = (uint32_t)(wn * 8192 + lane * 16);
+    const int sixteen = (kq & 1) * 2 + (kq >> 1);            // the columns that weight_operand gives this lane
+    const uint32_t po0 = (uint32_t)((sixteen ^ (nl & 7)) * 16), po1 = (uint32_t)(((4 + sixteen) ^ (nl & 7)) * 16);
+    int4_t aop[2][2][2];                                     // of two phases, row block, half
+    int4_t bop[2][4];                                        // half, tile row
+    u32x4_t raw[2][4];
+    auto read_a = [&](int u, int ph, int b) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            aop[ph & 1][b][i] = *reinterpret_cast<const int4_t*>(stage_a(u % SA) + a_rd + (ph * 2 + b) * 2048 + (i ? po1 : po0));
+    };
+    auto read_b = [&](int u, int r) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) raw[i][r] = *reinterpret_cast<const u32x4_t*>(stage_b(u % SB) + b_rd + r * 2048 + i * 1024);
+    };
+
+    auto step = [&](int u, int t) {
+#pragma unroll
+        for (int ph = 0; ph < PH; ++ph) {
+            if (ph == PH - 1) {
+                wait_and_barrier<(SA - 2) * NA + (SB - 2) * NB>();           // the next step's tiles have landed
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            auto mfma = [&](int b, int r) {
+#pragma unroll
+                for (int i = 0; i < 2; ++i) acc[ph * 2 + b][r] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bop[i][r], aop[ph & 1][b][i], acc[ph * 2 + b][r], 0, 0, 0);
+            };
+            for (int b = 0; b < 2; ++b) read_a(ph == PH - 1 ? u + 1 : u, ph == PH - 1 ? 0 : ph + 1, b);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (ph == 0) {
+                    bop[0][r] = weight_operand(raw[0][r]);
+                    bop[1][r] = weight_operand(raw[1][r]);
+                }
+                mfma(r & 1, r);
+                mfma(~r & 1, r);
+                if (ph == PH - 1) read_b(u + 1, r);
+            }
+            const int pa = (ph + 1) % PH;                     // phases since the barrier
+            int vm = 0;
+            const int fu = pa == 0 ? u : u + U - 1, ft = pa == 0 ? t : t - 1;    // the step whose stage that barrier freed
+            if (pa < AP) {
+#pragma unroll
+                for (int k = pa * NA / AP; k < (pa + 1) * NA / AP; ++k) a_dma(fu % SA, ft + SA, k);
+                vm += NA / AP;
+                __builtin_amdgcn_sched_barrier(0x78F);       // everything but memory loads may cross: the counted waits rely on their order
+            }
+            if (BP == 0 ? pa == 0 : pa >= BP) {
+                constexpr int EACH = BP == 0 ? NB : NB / (PH - BP);
+#pragma unroll
+                for (int k = (pa - BP) * EACH; k < (pa - BP + 1) * EACH; ++k) b_dma(fu % SB, ft + SB, k);
+                vm += EACH;
+            }
+            if (ph == 0) __builtin_amdgcn_sched_group_barrier(0x002, 12, 0);
+#pragma unroll
+            for (int g = 0; g < 8; ++g) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+                if (ph == PH - 1) {
+                    if (g < 2) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                    if (g & 1) __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+                } else if (g < 4) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                if (ph == 0 && g < 6) __builtin_amdgcn_sched_group_barrier(0x002, 6, 0);
+                if (g < vm) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    // the requests of the steps before the first one, in the order of the loop (its waits are counts)
+#pragma unroll
+    for (int k = 0; k < (SB > SA ? NB : 0); ++k) b_dma(0, 0, k);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int v = 0; v < SA; ++v) {
+#pragma unroll
+        for (int k = 0; k < (v == SA - 1 ? NA / AP : NA); ++k) a_dma(v, v, k);       // (the rest, in the first step)
+        __builtin_amdgcn_sched_barrier(0);
+        if (v < SA - 1 || BP == 0)
+#pragma unroll
+            for (int k = 0; k < NB; ++k) b_dma(v + SB - SA, v + SB - SA, k);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+    wait_and_barrier<(SA - 2) * NA + NA / AP + (SB - (BP == 0 ? 1 : 2)) * NB>();
+    for (int b = 0; b < 2; ++b) read_a(0, 0, b);
+#pragma unroll
+    for (int r = 0; r < 4; ++r) read_b(0, r);
+    __builtin_amdgcn_sched_barrier(0);
+
+    for (int t = 0;; t += U) {            // T is even; leaving between two steps keeps every wait inside an exact count
+        bool done = false;
+#pragma unroll
+        for (int u = 0; u < U; u += 2) {
+            step(u, t + u);
+            step(u + 1, t + u + 1);
+            if (t + u + 2 >= T) {
+                done = true;
+                break;
+            }
+        }
+        if (done) break;
+    }
+    wait_and_barrier<0>();                // no load into LDS outlives the workgroup
+
+    // a lane holds row 16 b + nl and the four columns 16 r + 4 kq + e
+    if (p.split > 1) {
+#pragma unroll
+        for (int b = 0; b < MBW; ++b) {
+            const int m = m0 + wm * (TM / 2) + b * 16 + nl;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int n = n0 + wn * 64 + r * 16 + kq * 4;
+                if (m < p.M && n < p.N) *reinterpret_cast<int4_t*>(p.ws + ((int64_t)z * p.M + m) * p.N + n) = acc[b][r];
+            }
+        }
+        return;
+    }
+    // results change lanes through the wavefront's own part of LDS, 16 rows x 128 bytes at a time, so that a store writes whole 128-byte runs
+    half4_t scale[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) scale[r] = *reinterpret_cast<const half4_t*>(p.scales + min(n0 + wn * 64 + r * 16, p.N - 16) + kq * 4);
+    uint8_t* const mine = lds_b0 + wave * 2048;
+#pragma unroll
+    for (int b = 0; b < MBW; ++b) {
+        const float row_scale = p.a_scales[min(m0 + wm * (TM / 2) + b * 16 + nl, p.M - 1)];
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            *reinterpret_cast<u32x2_t*>(mine + nl * 128 + (((r * 2 + (kq >> 1)) ^ (nl & 7)) * 16) + (kq & 1) * 8) = four_results<TYPE>(acc[b][r], row_scale, scale[r]);
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int row = h * 8 + (lane >> 3), piece = lane & 7;
+            const u32x4_t v = *reinterpret_cast<const u32x4_t*>(mine + row * 128 + ((piece ^ (row & 7)) * 16));
+            const int m = m0 + wm * (TM / 2) + b * 16 + row, n = n0 + wn * 64 + piece * 8;
+            if (m < p.M && n < p.N) __builtin_nontemporal_store(v, reinterpret_cast<u32x4_t*>(static_cast<half_t*>(p.C) + (int64_t)m * p.N + n));
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
     }
 }
 
@@ -137,7 +349,7 @@ __global__ __launch_bounds__(256) void w8a8_join_kernel(const W8A8Params p) {
     int4_t s = *reinterpret_cast<const int4_t*>(p.ws + at);
     for (int z = 1; z < p.split; ++z) s += *reinterpret_cast<const int4_t*>(p.ws + z * all + at);
     const int m = (int)(at / p.N), c = (int)(at - (int64_t)m * p.N);
-    *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, p.a_scales[m], p.scales + c);
+    *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, p.a_scales[m], *reinterpret_cast<const half4_t*>(p.scales + c));
 }
 
 constexpr int kCompute = 256;                                // compute units
@@ -145,11 +357,23 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 
 struct W8A8Plan {
     int mb, nt, wk, split;
+    bool tile;
     int64_t XB, YB;
+    int64_t workgroups() const { return (tile ? (XB * YB + kXcds - 1) / kXcds * kXcds : XB * YB) * split; }
+    int threads() const { return tile ? kTileThreads : wk * 64; }
 };
 
 static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
     W8A8Plan p;
+    p.tile = M > 128;
+    if (p.tile) {
+        p.mb = M > 256 ? 8 : 4;
+        p.XB = (N + kTileN - 1) / kTileN;
+        p.YB = (M + 32 * p.mb - 1) / (32 * p.mb);
+        const int64_t most = std::min<int64_t>({8, K / 256, (int64_t)(std::min(workspace, kW8A8Workspace) / ((size_t)M * N * 4))});
+        p.split = (int)std::max<int64_t>(1, std::min<int64_t>(most, kCompute / (p.XB * p.YB)));
+        return p;
+    }
     p.mb = M <= 16 ? 1 : M <= 32 ? 2 : 4;
     p.nt = p.mb == 1 ? 1 : 2;
     p.wk = 8;
@@ -167,8 +391,10 @@ static rtn_status check_w8a8(int64_t M, int64_t N, int64_t K) {
 
 template <int TYPE>
 static hipError_t launch_w8a8(W8A8Params p, const W8A8Plan& plan, hipStream_t st) {
-    const dim3 grid((unsigned)(plan.XB * plan.YB * plan.split)), block(plan.wk * 64);
-    if (plan.mb == 1) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 1, 1, 8, 4>), grid, block, 0, st, p);
+    const dim3 grid((unsigned)plan.workgroups()), block(plan.threads());
+    if (plan.tile && plan.mb == 8) hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, 8>), grid, block, 0, st, p);
+    else if (plan.tile) hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, 4>), grid, block, 0, st, p);
+    else if (plan.mb == 1) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 1, 1, 8, 4>), grid, block, 0, st, p);
     else if (plan.mb == 2) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 2, 2, 8, 4>), grid, block, 0, st, p);
     else hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 4, 2, 8, 4>), grid, block, 0, st, p);
     hipError_t e = hipGetLastError();
@@ -198,8 +424,7 @@ extern "C" rtn_status rtn_linear_w8a8(const void* dev_q, const float* dev_q_scal
     if (!rtn::aligned_to(dev_q_scales, 4)) return RTN_ERR_ALIGN;
     if (M == 0) return RTN_OK;
     const rtn::W8A8Plan plan = rtn::w8a8_plan(M, N, K, dev_workspace ? workspace_nbytes : 0);
-    if (!rtn::launchable(plan.XB * plan.YB * plan.split, plan.wk * 64) || 
-        (plan.split > 1 && !rtn::launchable((M * N / 4 + 255) / 256, 256)))
+    if (!rtn::launchable(plan.workgroups(), plan.threads()) || (plan.split > 1 && !rtn::launchable((M * N / 4 + 255) / 256, 256)))
         return RTN_ERR_SHAPE;
     const rtn::W8A8Params p = {static_cast<const int8_t*>(dev_q), dev_q_scales, static_cast<const uint8_t*>(dev_qweight), static_cast<const rtn::half_t*>(dev_scales),
                                dev_C, static_cast<int*>(dev_workspace), (int)M, (int)N, (int)(K / 64), (int)plan.XB, (int)plan.YB, plan.split};
