@@ -2,23 +2,24 @@
 // rows, quantised with a scale for each token (or, the first two, left in 16 bits).
 //
 // Every one of them is v_k times a factor of the row: v = h w with the factor rsqrt(mean(h^2) + eps) for the norm, v = act(a) b and v = x
-// with 1.  The largest |v| and the sum of squares are found in one sweep and the codes are rne(v * 127 / max|v|), which the factor does not
+// with 1.  The largest |v| and the sum of squares are found in one sweep and the codes are rne(v / (max|v| / 127)), which the factor does not
 // enter; so a row is read once, kept in registers, and meets once over the workgroup, not once for the norm and again for the scale.
-// h w is exact in fp32 (two significands of at most 11 bits), so a code is the exact product's rounding by one reciprocal of 24 bits.
+// h w is exact in fp32 (two significands of at most 11 bits); every other step is one rounding in fp32, in the order that the header of the entry points
+// gives, so that the codes of plain and normed rows are what the same steps give anywhere else.
 //
 // Bound by memory: the norm with a residual moves 7 bytes an element quantised, the gated activation 5, plain rows 3.
 #include "rtn_paged.h"
 
 namespace rtn {
 
-enum { ROW_PLAIN = 0, ROW_NORM = 1, ROW_GATED = 2 };
+enum { ROW_PLAIN, ROW_NORM, ROW_SILU, ROW_GELU };
 
 struct RowParams {
     const void *x, *residual, *weight;
     void *sum, *out;
     float* scales;
     int64_t x_stride, residual_stride, sum_stride;
-    int rows, dim, gelu;
+    int rows, dim;
     float eps, inv_dim;
 };
 
@@ -41,17 +42,35 @@ __device__ __forceinline__ float wave_largest(float x) {
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// act(a) b.  Both activations are a / (1 + exp(-z)): z = a, or a sqrt(8 / pi) (1 + 0.044715 a^2), for which it is a / 2 (1 + tanh(z / 2)).
-__device__ __forceinline__ float gated(float a, float b, bool gelu) {
-    const float z = gelu ? a * fmaf(a * a, 0.071354816f, 1.5957691f) : a;
-    return a * __builtin_amdgcn_rcpf(1.0f + expf(-z)) * b;
+#pragma clang fp contract(off)
+
+// exp(x) = 2^n 2^f with x log2(e) = n + f: the product's rounding and log2(e)'s second part go into f.  No special cases within +-88.
+__device__ __forceinline__ float exp_within_88(float x) {
+    const float t = x * 1.44269504f, n = __builtin_rintf(t);
+    const float rest = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269504f, -t));
+    return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(t - n + rest), (int)n);
 }
 
-// Four codes of values within +-127: adding 1.5 2^23 rounds to nearest even and leaves the code in the lowest byte.
+// a / d, rounded as a division is, for d >= 1: a reciprocal and a quotient with a step of correction each (5 instructions, 10 with the scaling
+// that a division of any two numbers needs).
+__device__ __forceinline__ float quotient(float a, float d) {
+    const float r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.0f), r0, r0), q = a * r;
+    return fmaf(fmaf(-d, q, a), r, q);
+}
+
+// act(a) b.  Both activations are a / (1 + exp(-z)): z = a, or a (1 + 0.044715 a^2) sqrt(8 / pi), for which it is a / 2 (1 + tanh(z / 2)).  (At z = -88
+// the quotient is 2^-120; there it may as well stay.)
+template <bool GELU>
+__device__ __forceinline__ float gated(float a, float b) {
+    const float z = GELU ? a * (1.0f + 0.044715f * a * a) * 1.59576912f : a;
+    return quotient(a, 1.0f + exp_within_88(__builtin_amdgcn_fmed3f(-z, -88.0f, 88.0f))) * b;
+}
+
+// Four codes of v * inv within +-127: adding 1.5 2^23 rounds to nearest even and leaves the code in the lowest byte.
 __device__ __forceinline__ uint32_t four_codes(const float* v, float inv) {
     uint32_t t[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) t[i] = __builtin_bit_cast(uint32_t, fmaf(v[i], inv, 12582912.0f));
+    for (int i = 0; i < 4; ++i) t[i] = __builtin_bit_cast(uint32_t, v[i] * inv + 12582912.0f);
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], 0x0C0C0400u), __builtin_amdgcn_perm(t[1], t[0], 0x0C0C0400u), 0x05040100u);
 }
 
@@ -61,6 +80,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams
     typedef typename Elem<TYPE>::one E;
     typedef typename Elem<TYPE>::x8 E8;
     constexpr int ROWS = T < 256 ? 256 / T : 1, WAVES = T / 64;
+    constexpr bool GATED = OP == ROW_SILU || OP == ROW_GELU;
     __shared__ float part[2][WAVES];
     const int t = threadIdx.x % T, row = (int)blockIdx.x * ROWS + (int)threadIdx.x / T;
     if (row >= p.rows) return;                               // (a whole wavefront; with more wavefronts a row there is one row)
@@ -68,20 +88,20 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams
     // Everything is requested before the first store (which may be to the same memory).  What is kept for the second sweep: the elements, the
     // norm's with its weight; of the gated activation the values, whose exponentials are not formed twice.
     E8 in[C], with[C], weight[OP == ROW_NORM ? C : 1];
-    float kept[OP == ROW_GATED ? C : 1][8];
+    float kept[GATED ? C : 1][8];
 #pragma unroll
     for (int c = 0; c < C; ++c) {
         const int k = (c * T + t) * 8;
         if (k >= p.dim) continue;
         in[c] = *reinterpret_cast<const E8*>(x + k);
-        if constexpr (OP == ROW_GATED) with[c] = *reinterpret_cast<const E8*>(x + p.dim + k);
+        if constexpr (GATED) with[c] = *reinterpret_cast<const E8*>(x + p.dim + k);
         if constexpr (OP == ROW_NORM) {
             if (p.residual) with[c] = *reinterpret_cast<const E8*>(static_cast<const E*>(p.residual) + row * p.residual_stride + k);
             weight[c] = *reinterpret_cast<const E8*>(static_cast<const E*>(p.weight) + k);
         }
     }
     auto value = [&](int c, int i) -> float {
-        if constexpr (OP == ROW_GATED) return kept[c][i];
+        if constexpr (GATED) return kept[c][i];
         else if constexpr (OP == ROW_NORM) return (float)in[c][i] * (float)weight[c][i];
         else return (float)in[c][i];
     };
@@ -101,7 +121,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams
         for (int i = 0; i < 8; ++i) {
             const float a = (float)in[c][i];
             if constexpr (OP == ROW_NORM) square = fmaf(a, a, square);
-            if constexpr (OP == ROW_GATED) kept[c][i] = gated(a, (float)with[c][i], p.gelu);
+            if constexpr (GATED) kept[c][i] = gated<OP == ROW_GELU>(a, (float)with[c][i]);
             if constexpr (QUANT) most = larger(most, fabsf(value(c, i)));
         }
     }
@@ -129,8 +149,9 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams
     float inv = 0.f;
     if constexpr (QUANT) {
         const bool none = most < kLeastRow;
-        inv = none ? 0.f : 127.0f / most;
-        if (t == 0) p.scales[row] = none ? 0.f : most * factor / 127.0f;
+        const float step = most * (1.0f / 127.0f);
+        inv = none ? 0.f : 1.0f / step;
+        if (t == 0) p.scales[row] = none ? 0.f : step * factor;
     }
 #pragma unroll
     for (int c = 0; c < C; ++c) {
@@ -227,7 +248,7 @@ extern "C" rtn_status rtn_norm_rows(const void* dev_x, int64_t rows, int64_t x_s
     if (!(eps >= 0.f)) return RTN_ERR_CONFIG;
     if (rows == 0) return RTN_OK;
     const rtn::RowParams p = {dev_x, dev_residual, dev_weight, dev_residual_out, dev_q ? dev_q : dev_out, dev_q_scales, x_stride, residual_stride,
-                              residual_out_stride, (int)rows, (int)dim, 0, eps, 1.0f / (float)dim};
+                              residual_out_stride, (int)rows, (int)dim, eps, 1.0f / (float)dim};
     return dev_q ? rtn::launch_typed<rtn::ROW_NORM, true>(p, dtype, stream) : rtn::launch_typed<rtn::ROW_NORM, false>(p, dtype, stream);
 }
 
@@ -239,9 +260,9 @@ extern "C" rtn_status rtn_gated_rows(const void* dev_x, int64_t rows, int64_t x_
     if (st != RTN_OK) return st;
     if (activation != RTN_ACT_SILU && activation != RTN_ACT_GELU_TANH) return RTN_ERR_CONFIG;
     if (rows == 0) return RTN_OK;
-    const rtn::RowParams p = {dev_x, nullptr, nullptr, nullptr, dev_q ? dev_q : dev_out, dev_q_scales, x_stride, 0, 0, (int)rows, (int)dim,
-                              activation == RTN_ACT_GELU_TANH, 0.f, 0.f};
-    return dev_q ? rtn::launch_typed<rtn::ROW_GATED, true>(p, dtype, stream) : rtn::launch_typed<rtn::ROW_GATED, false>(p, dtype, stream);
+    const rtn::RowParams p = {dev_x, nullptr, nullptr, nullptr, dev_q ? dev_q : dev_out, dev_q_scales, x_stride, 0, 0, (int)rows, (int)dim, 0.f, 0.f};
+    if (activation == RTN_ACT_SILU) return dev_q ? rtn::launch_typed<rtn::ROW_SILU, true>(p, dtype, stream) : rtn::launch_typed<rtn::ROW_SILU, false>(p, dtype, stream);
+    return dev_q ? rtn::launch_typed<rtn::ROW_GELU, true>(p, dtype, stream) : rtn::launch_typed<rtn::ROW_GELU, false>(p, dtype, stream);
 }
 
 extern "C" rtn_status rtn_quantize_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, void* dev_q, float* dev_q_scales, void* stream) {
@@ -249,7 +270,7 @@ extern "C" rtn_status rtn_quantize_rows(const void* dev_x, int64_t rows, int64_t
     rtn_status st = rtn::check_outputs(rows, dim, dtype, nullptr, dev_q, dev_q_scales);
     if (st == RTN_OK) st = rtn::check_rows(dev_x, x_stride, dim);
     if (st != RTN_OK || rows == 0) return st;
-    const rtn::RowParams p = {dev_x, nullptr, nullptr, nullptr, dev_q, dev_q_scales, x_stride, 0, 0, (int)rows, (int)dim, 0, 0.f, 0.f};
+    const rtn::RowParams p = {dev_x, nullptr, nullptr, nullptr, dev_q, dev_q_scales, x_stride, 0, 0, (int)rows, (int)dim, 0.f, 0.f};
     return rtn::launch_typed<rtn::ROW_PLAIN, true>(p, dtype, stream);
 }
 

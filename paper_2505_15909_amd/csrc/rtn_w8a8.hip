@@ -5,6 +5,9 @@
 // bring the eights of neighbouring quarters together, so that quarters 0 .. 3 hold the sixteens 0, 2, 1, 3, which are 16 bytes in a row of
 // row-major activations; four v_xor take the 128 off.
 #include <algorithm>
+#include <array>
+#include <cmath>
+#include <utility>
 
 #include "rtn_paged.h"
 
@@ -40,6 +43,10 @@ struct W8A8Params {
     int XB, YB, split;      // workgroups along N, along M, along K
 };
 
+constexpr int kBufferFlags = 0x00020000;
+constexpr uint32_t kNoRow = 0x80000000u;                     // beyond every resource: reads zeros
+constexpr int kStreaming = 2;                                // read once
+
 // ---- Few rows: bound by the stream of weights.  A wavefront multiplies NT tile rows of weights by MB blocks of 16 rows, both straight
 // from memory into registers, D tiles ahead; the WK wavefronts of a workgroup take the tiles of its K range in turn (what they read
 // together is in one piece), and add up in LDS. ----
@@ -55,14 +62,17 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
     const int t0 = (int)((int64_t)p.KT * z / p.split), t1 = (int)((int64_t)p.KT * (z + 1) / p.split);
     const int n = max(0, (t1 - t0 - wave + WK - 1) / WK);    // this wavefront's tiles: t0 + wave + WK i
 
-    const int m0 = y * (16 * MB), rows16 = p.N / 16, K = p.KT * 64;
-    const int8_t* a_at[MB];
-    const uint8_t* b_at[NT];
+    // Through resources that start at this workgroup's rows: rows past M or N read zeros, at no cost.
+    const int m0 = y * (16 * MB), K = p.KT * 64, a_rows = min(16 * MB, p.M - m0), b_tiles = min(NT, p.N / 16 - x * NT);
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.A) + (int64_t)m0 * K, 0, (uint32_t)a_rows * (uint32_t)K, kBufferFlags);
+    const __amdgpu_buffer_rsrc_t rb =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.B) + (int64_t)x * NT * p.KT * 1024, 0, (uint32_t)b_tiles * (uint32_t)p.KT * 1024u, kBufferFlags);
+    uint32_t a_at[MB], b_at[NT];
 #pragma unroll
-    for (int i = 0; i < MB; ++i)                             // rows beyond M: the last one, not stored
-        a_at[i] = p.A + (int64_t)min(m0 + 16 * i + nl, p.M - 1) * K + ((kq & 1) * 2 + (kq >> 1)) * 16;
+    for (int i = 0; i < MB; ++i)
+        a_at[i] = 16 * i + nl < a_rows ? (uint32_t)(16 * i + nl) * (uint32_t)K + ((kq & 1) * 2 + (kq >> 1)) * 16 : kNoRow;
 #pragma unroll
-    for (int j = 0; j < NT; ++j) b_at[j] = p.B + ((int64_t)min(x * NT + j, rows16 - 1) * p.KT) * 1024 + lane * 16;
+    for (int j = 0; j < NT; ++j) b_at[j] = j < b_tiles ? (uint32_t)j * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
 
     int4_t acc[MB][NT];
 #pragma unroll
@@ -72,11 +82,11 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
     int4_t a[D][MB];
     u32x4_t w[D][NT];
     auto load = [&](int s, int i) {
-        const int64_t t = t0 + wave + WK * min(i, n - 1);
+        const int t = t0 + wave + WK * min(i, n - 1);
 #pragma unroll
-        for (int j = 0; j < NT; ++j) w[s][j] = load_stream16(b_at[j] + t * 1024);
+        for (int j = 0; j < NT; ++j) w[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, b_at[j], t * 1024, kStreaming);
 #pragma unroll
-        for (int k = 0; k < MB; ++k) a[s][k] = *reinterpret_cast<const int4_t*>(a_at[k] + t * 64);
+        for (int k = 0; k < MB; ++k) a[s][k] = __builtin_bit_cast(int4_t, __builtin_amdgcn_raw_buffer_load_b128(ra, a_at[k], t * 64, 0));
     };
     auto multiply = [&](int s) {
 #pragma unroll
@@ -135,8 +145,6 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
 // the one barrier of a step stands before its last phase, whose operands are in registers by then: the stage is free behind it, and the
 // requests for it go out over the phases that follow. ----
 constexpr int kTileN = 256, kTileThreads = 512;
-constexpr int kBufferFlags = 0x00020000;
-constexpr uint32_t kNoRow = 0x80000000u;                     // beyond every resource: reads zeros
 constexpr int kZGroup = 4;
 
 // 16 bytes per lane from global memory into 1 KiB of LDS at a wave-uniform address
@@ -341,6 +349,130 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
     }
 }
 
+// ---- Rows between: bound by the stream of weights where enough of them is on its way.  The eight wavefronts of a workgroup stand 8 / WK along N and WK along K.
+// A wavefront has NT tile rows of weights, straight into registers; the activations, 16 MB rows, come into LDS once for the wavefronts along N.
+// A step is 128 columns for each wavefront along K; both are requested S - 1 steps ahead, and one barrier a step says that its activations have landed
+// and the last one's are used up.  The wavefronts along K add up in LDS at the end. ----
+template <int TYPE, int MB, int NT, int WK, int S>
+__global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) void w8a8_block_kernel(const W8A8Params p) {
+    constexpr int WN = 8 / WK, NA = MB * WK / 4, EACH = NA + 2 * NT;         // requests of a wavefront and step: of activations, in all
+    constexpr int A_BYTES = MB * WK * 2048;
+    static_assert(MB * NT * 8192 * (WK - 1) / WK <= 2 * A_BYTES, "sums of the wavefronts along K");
+    __shared__ __align__(16) uint8_t lds0[A_BYTES], lds1[A_BYTES], lds2[A_BYTES], lds3[S > 3 ? A_BYTES : 16];
+    auto stage = [&](int i) { return i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3; };
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nl = lane & 15, kq = lane >> 4;
+    const int wn = wave % WN, wk = wave / WN;
+    const int blocks = (p.XB * p.YB + kXcds - 1) / kXcds * kXcds, z = blockIdx.x / blocks;
+    int xb, yb;
+    if (!xcd_tile((int)blockIdx.x - z * blocks, p.XB, p.YB, kZGroup, &xb, &yb)) return;
+    const int m0 = yb * (16 * MB), K = p.KT * 64, tile0 = (xb * WN + wn) * NT;
+    const int s0 = (int)((int64_t)(p.KT / 2) * z / p.split), units = (int)((int64_t)(p.KT / 2) * (z + 1) / p.split) - s0;      // of 128 columns
+    const int T = (units + WK - 1) / WK;
+
+    const int a_rows = min(16 * MB, p.M - m0), b_tiles = __builtin_amdgcn_readfirstlane(max(0, min(NT, p.N / 16 - tile0)));      // (none: a wavefront beyond N)
+    const int first = __builtin_amdgcn_readfirstlane(min(tile0, p.N / 16 - 1));
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(p.A) + (int64_t)m0 * K, 0, (uint32_t)a_rows * (uint32_t)K, kBufferFlags);
+    const __amdgpu_buffer_rsrc_t rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.B) + (int64_t)first * p.KT * 1024, 0,
+                                                                        (uint32_t)b_tiles * (uint32_t)p.KT * 1024u, kBufferFlags);
+    uint32_t a_lane[NA], b_lane[NT];
+    int a_unit[NA];                                          // request i of the wavefront: eight rows of the activations of wavefronts a_unit along K
+#pragma unroll
+    for (int i = 0; i < NA; ++i) {
+        const int r = wave * NA + i, row = r % (2 * MB) * 8 + (lane >> 3);
+        a_unit[i] = r / (2 * MB);
+        a_lane[i] = row < a_rows ? (uint32_t)row * (uint32_t)K + ((lane & 7) ^ (lane >> 3)) * 16 : kNoRow;
+    }
+#pragma unroll
+    for (int j = 0; j < NT; ++j) b_lane[j] = j < b_tiles ? (uint32_t)j * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
+
+    u32x4_t w[S][NT][2];
+    auto request = [&](int u, int t) {                       // step t, into stage and registers u; units past the last one: the last, not multiplied
+#pragma unroll
+        for (int i = 0; i < NA; ++i) load_to_lds(ra, stage(u) + (wave * NA + i) * 1024, a_lane[i], (s0 + min(t * WK + a_unit[i], units - 1)) * 128);
+        const int at = s0 + min(t * WK + wk, units - 1);
+#pragma unroll
+        for (int j = 0; j < NT; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) w[u][j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, b_lane[j], at * 2048 + h * 1024, kStreaming);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    int4_t acc[MB][NT];
+#pragma unroll
+    for (int b = 0; b < MB; ++b)
+#pragma unroll
+        for (int j = 0; j < NT; ++j) acc[b][j] = (int4_t){0, 0, 0, 0};
+    const int sixteen = (kq & 1) * 2 + (kq >> 1);
+    const uint32_t a_rd = (uint32_t)(wk * MB * 2048 + nl * 128), po[2] = {(uint32_t)((sixteen ^ (nl & 7)) * 16), (uint32_t)(((4 + sixteen) ^ (nl & 7)) * 16)};
+    auto step = [&](int u, int t) {
+        __builtin_amdgcn_sched_barrier(0);
+        wait_and_barrier<(S - 2) * EACH>();
+        __builtin_amdgcn_sched_barrier(0);
+        request((u + S - 1) % S, t + S - 1);
+        if (WK > 1 && t * WK + wk >= units) return;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            int4_t wj[NT];
+#pragma unroll
+            for (int j = 0; j < NT; ++j) wj[j] = weight_operand(w[u][j][h]);
+#pragma unroll
+            for (int b = 0; b < MB; ++b) {
+                const int4_t a = *reinterpret_cast<const int4_t*>(stage(u) + a_rd + b * 2048 + po[h]);
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[b][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(wj[j], a, acc[b][j], 0, 0, 0);
+            }
+        }
+    };
+#pragma unroll
+    for (int v = 0; v < S - 1; ++v) request(v, v);
+    // whole turns, then what is left: an exit within a turn would be, to the compiler's counts of loads, one more way into the next
+    int t = 0;
+    for (; t + S <= T; t += S) {
+#pragma unroll
+        for (int u = 0; u < S; ++u) step(u, t + u);
+    }
+    const int left = T - t;
+#pragma unroll
+    for (int u = 0; u < S - 1; ++u)
+        if (u < left) step(u, t + u);
+    wait_and_barrier<0>();                // no load into LDS outlives the workgroup
+
+    if constexpr (WK > 1) {
+        // half of the row blocks in one stage, half in the other; the first wavefront along K adds the others' sums to its own
+        auto place = [&](int k, int b, int j) {
+            uint8_t* const half = b < MB / 2 ? lds0 : lds1;
+            return reinterpret_cast<int4_t*>(half + ((((k - 1) * WN + wn) * (MB / 2) + b % (MB / 2)) * NT + j) * 1024 + lane * 16);
+        };
+        if (wk > 0) {
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) *place(wk, b, j) = acc[b][j];
+        }
+        __syncthreads();
+        if (wk > 0) return;
+#pragma unroll
+        for (int k = 1; k < WK; ++k)
+#pragma unroll
+            for (int b = 0; b < MB; ++b)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[b][j] += *place(k, b, j);
+    }
+    // a lane holds row 16 b + nl and the four columns 16 j + 4 kq + e
+#pragma unroll
+    for (int j = 0; j < NT; ++j) {
+        const int n = (tile0 + j) * 16 + kq * 4;
+        if (n >= p.N) continue;
+        const half4_t scale = *reinterpret_cast<const half4_t*>(p.scales + n);
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            const int m = m0 + b * 16 + nl;
+            if (m >= p.M) continue;
+            if (p.split > 1) *reinterpret_cast<int4_t*>(p.ws + ((int64_t)z * p.M + m) * p.N + n) = acc[b][j];
+            else *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + (int64_t)m * p.N + n) = four_results<TYPE>(acc[b][j], p.a_scales[m], scale);
+        }
+    }
+}
+
 // Sums of the K splits' parts, four columns a thread.
 template <int TYPE>
 __global__ __launch_bounds__(256) void w8a8_join_kernel(const W8A8Params p) {
@@ -352,36 +484,84 @@ __global__ __launch_bounds__(256) void w8a8_join_kernel(const W8A8Params p) {
     *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, p.a_scales[m], *reinterpret_cast<const half4_t*>(p.scales + c));
 }
 
-constexpr int kCompute = 256;                                // compute units
 constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 
+// The kernels' shapes and what their time is made of, in us.  Stream and block kernels: start + units x (workgroups on the fullest compute unit) x
+// (each + more x the share of a workgroup's rows that M has), a unit being the 64 (128) columns of a step of each wavefront along K: a compute unit
+// gets 50 to 65 GB/s out of the L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup a compute unit, whose step takes `each` where half
+// the chip is busy and `each + more` where all of it is (power).  That against the weights' stream, and a K split's join.  Fitted to 16 000 launches
+// over 900 problems (1 to 8192 rows, 256 to 57344 columns, K 1024 to 28672): 7 to 12 % rms, and the pick is 1.6 % behind the best of all launches on the mean.
+enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
+struct W8A8Shape {
+    int kind, mb, nt, wk, depth;
+    float start, each, more;
+};
+constexpr W8A8Shape kShapes[] = {
+    {W8A8_STREAM, 1, 1, 8, 4, 3.46f, 0.123f, 0.271f}, {W8A8_STREAM, 1, 1, 8, 2, 3.53f, 0.157f, 0.221f}, {W8A8_STREAM, 1, 2, 8, 2, 3.29f, 0.276f, 0.286f},
+    {W8A8_STREAM, 1, 4, 8, 2, 3.22f, 0.576f, 0.382f}, {W8A8_STREAM, 2, 2, 8, 2, 3.18f, 0.348f, 0.468f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.38f, 0.462f, 0.051f},
+    {W8A8_BLOCK, 2, 2, 4, 3, 3.54f, 0.831f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.06f, 0.699f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.54f, 0.519f, 0.283f},
+    {W8A8_BLOCK, 4, 1, 2, 3, 3.93f, 0.463f, 0.057f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.26f, 0.414f, 0.f},     {W8A8_BLOCK, 4, 2, 2, 3, 4.63f, 0.837f, 0.f},
+    {W8A8_BLOCK, 8, 2, 2, 3, 6.48f, 1.134f, 0.024f},  {W8A8_BLOCK, 8, 2, 1, 3, 6.58f, 0.917f, 0.f},     {W8A8_TILE, 4, 0, 0, 0, 6.17f, 0.724f, 0.170f},
+    {W8A8_TILE, 8, 0, 0, 0, 7.86f, 1.117f, 0.352f}};
+constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
+
 struct W8A8Plan {
-    int mb, nt, wk, split;
-    bool tile;
+    int shape, split;
     int64_t XB, YB;
-    int64_t workgroups() const { return (tile ? (XB * YB + kXcds - 1) / kXcds * kXcds : XB * YB) * split; }
-    int threads() const { return tile ? kTileThreads : wk * 64; }
+    int64_t workgroups() const { return (kShapes[shape].kind == W8A8_STREAM ? XB * YB : (XB * YB + kXcds - 1) / kXcds * kXcds) * split; }
 };
 
+constexpr int log2_const(int n) { return n > 1 ? 1 + log2_const(n / 2) : 0; }
+
+// What a shape covers, as powers of two: a workgroup's rows and columns, a unit's columns of K, wavefronts along K.
+struct W8A8Cover { int rows, columns, unit, along; };
+constexpr W8A8Cover cover_of(const W8A8Shape& k) {
+    return k.kind == W8A8_TILE ? W8A8Cover{log2_const(32 * k.mb), log2_const(kTileN), 8, 0}
+                               : W8A8Cover{log2_const(16 * k.mb), log2_const(k.kind == W8A8_BLOCK ? 128 * k.nt / k.wk : 16 * k.nt), k.kind == W8A8_BLOCK ? 7 : 6, log2_const(k.wk)};
+}
+template <int... I>
+constexpr std::array<W8A8Cover, sizeof...(I)> covers(std::integer_sequence<int, I...>) { return {cover_of(kShapes[I])...}; }
+constexpr auto kCovers = covers(std::make_integer_sequence<int, kShapeCount>());
+
+// (0.3 us for a few rows, 0.8 where most of the shapes are looked at.)
 static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
-    W8A8Plan p;
-    p.tile = M > 128;
-    if (p.tile) {
-        p.mb = M > 256 ? 8 : 4;
-        p.XB = (N + kTileN - 1) / kTileN;
-        p.YB = (M + 32 * p.mb - 1) / (32 * p.mb);
-        const int64_t most = std::min<int64_t>({8, K / 256, (int64_t)(std::min(workspace, kW8A8Workspace) / ((size_t)M * N * 4))});
-        p.split = (int)std::max<int64_t>(1, std::min<int64_t>(most, kCompute / (p.XB * p.YB)));
-        return p;
+    W8A8Plan plan = {};
+    float best = 1e30f;
+    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.12e6f);
+    const float s4 = stream * stream * stream * stream;
+    const int splits = (int)std::min(8.f, (float)std::min(workspace, kW8A8Workspace) * 0.25f / MN);      // (below 8 in all where that is near)
+    const int pieces = (int)((M + 15) / 16);
+    auto up = [](int64_t n, int log2) { return (n + ((int64_t)1 << log2) - 1) >> log2; };
+    for (int i = 0; i < kShapeCount; ++i) {
+        const W8A8Shape& k = kShapes[i];
+        const W8A8Cover& c = kCovers[i];
+        if ((1 << c.rows) >= 32 * pieces && c.rows > 5) continue;            // mostly rows beyond M
+        if (k.kind != W8A8_TILE && pieces > 8 << (c.rows - 4)) continue;     // the weights eight times and more
+        const int64_t XB = up(N, c.columns), YB = up(M, c.rows), tiles = XB * YB, all_units = K >> c.unit;
+        const float unit_us = k.each + k.more * (float)M / (float)(YB << c.rows);
+        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 2.45e6f));
+        for (int split = 1; split <= std::max(1, splits); ++split) {
+            if (split > 1 && ((split << c.along) > all_units || tiles * split > 800)) break;
+            const float steps = (float)up((uint32_t)(all_units + split - 1) / (uint32_t)split, c.along);
+            float work;
+            if (k.kind == W8A8_TILE) {
+                const int64_t on_xcd = up(tiles, 3) * split;
+                const float part = (float)(on_xcd & 31) * (1.f / 32.f);
+                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 5.3f) - 5.3f;
+                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 5.3f;
+            } else {
+                work = steps * unit_us * (float)(k.kind == W8A8_STREAM ? up(tiles * split, 8) : up(up(tiles, 3) * split, 5));
+            }
+            const float rest = once + (split > 1 ? 2.84f + (outputs + 4.f * outputs * (float)split) * (1.f / 6.12e6f) : 0.f);
+            if (rest + std::max(work, stream) >= best) continue;
+            const float t = rest + std::sqrt(std::sqrt(work * work * work * work + s4));
+            if (t < best) {
+                best = t;
+                plan = {i, split, XB, YB};
+            }
+        }
     }
-    p.mb = M <= 16 ? 1 : M <= 32 ? 2 : 4;
-    p.nt = p.mb == 1 ? 1 : 2;
-    p.wk = 8;
-    p.XB = (N / 16 + p.nt - 1) / p.nt;
-    p.YB = (M + 16 * p.mb - 1) / (16 * p.mb);
-    const int64_t most = std::min<int64_t>({16, K / 64 / p.wk, (int64_t)(std::min(workspace, kW8A8Workspace) / ((size_t)M * N * 4))});
-    p.split = (int)std::max<int64_t>(1, std::min<int64_t>(most, kCompute / (p.XB * p.YB)));
-    return p;
+    return plan;
 }
 
 static rtn_status check_w8a8(int64_t M, int64_t N, int64_t K) {
@@ -389,14 +569,22 @@ static rtn_status check_w8a8(int64_t M, int64_t N, int64_t K) {
     return RTN_OK;
 }
 
+template <int TYPE, int I>
+static void launch_shape(const W8A8Params& p, dim3 grid, hipStream_t st) {
+    constexpr W8A8Shape k = kShapes[I];
+    if constexpr (k.kind == W8A8_STREAM) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, k.mb, k.nt, k.wk, k.depth>), grid, dim3(k.wk * 64), 0, st, p);
+    else if constexpr (k.kind == W8A8_BLOCK) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, k.depth>), grid, dim3(512), 0, st, p);
+    else hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, k.mb>), grid, dim3(kTileThreads), 0, st, p);
+}
+
+template <int TYPE, int... I>
+static void launch_one_of(std::integer_sequence<int, I...>, int shape, const W8A8Params& p, dim3 grid, hipStream_t st) {
+    (void)((shape == I && (launch_shape<TYPE, I>(p, grid, st), true)) || ...);
+}
+
 template <int TYPE>
-static hipError_t launch_w8a8(W8A8Params p, const W8A8Plan& plan, hipStream_t st) {
-    const dim3 grid((unsigned)plan.workgroups()), block(plan.threads());
-    if (plan.tile && plan.mb == 8) hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, 8>), grid, block, 0, st, p);
-    else if (plan.tile) hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, 4>), grid, block, 0, st, p);
-    else if (plan.mb == 1) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 1, 1, 8, 4>), grid, block, 0, st, p);
-    else if (plan.mb == 2) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 2, 2, 8, 4>), grid, block, 0, st, p);
-    else hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, 4, 2, 8, 4>), grid, block, 0, st, p);
+static hipError_t launch_w8a8(const W8A8Params& p, const W8A8Plan& plan, hipStream_t st) {
+    launch_one_of<TYPE>(std::make_integer_sequence<int, kShapeCount>(), plan.shape, p, dim3((unsigned)plan.workgroups()), st);
     hipError_t e = hipGetLastError();
     if (e == hipSuccess && p.split > 1) {
         hipLaunchKernelGGL((w8a8_join_kernel<TYPE>), dim3((unsigned)(((int64_t)p.M * p.N / 4 + 255) / 256)), dim3(256), 0, st, p);
@@ -424,7 +612,7 @@ extern "C" rtn_status rtn_linear_w8a8(const void* dev_q, const float* dev_q_scal
     if (!rtn::aligned_to(dev_q_scales, 4)) return RTN_ERR_ALIGN;
     if (M == 0) return RTN_OK;
     const rtn::W8A8Plan plan = rtn::w8a8_plan(M, N, K, dev_workspace ? workspace_nbytes : 0);
-    if (!rtn::launchable(plan.workgroups(), plan.threads()) || (plan.split > 1 && !rtn::launchable((M * N / 4 + 255) / 256, 256)))
+    if (!rtn::launchable(plan.workgroups(), 512) || (plan.split > 1 && !rtn::launchable((M * N / 4 + 255) / 256, 256)))
         return RTN_ERR_SHAPE;
     const rtn::W8A8Params p = {static_cast<const int8_t*>(dev_q), dev_q_scales, static_cast<const uint8_t*>(dev_qweight), static_cast<const rtn::half_t*>(dev_scales),
                                dev_C, static_cast<int*>(dev_workspace), (int)M, (int)N, (int)(K / 64), (int)plan.XB, (int)plan.YB, plan.split};

@@ -3,13 +3,12 @@
 
 Tolerances.  u is the unit roundoff of the element type (2^-11 fp16, 2^-8 bf16), e = 2^-24 that of fp32; fp16 results below the normal range are off by
 up to 2^-25.
-  Codes of plain and normed rows are exact: the values (x, or h w with two significands of at most 11 bits) and the largest of them are exact in fp32, the
-  reciprocal 127 / max is one IEEE division, and value times reciprocal is rounded once, to nearest even: a reference in 64 bits finds the same.
-  Plain scales are one IEEE division: exact.
+  Codes of plain and normed rows are exact: the values (x, or h w with two significands of at most 11 bits) and the largest of them are exact in fp32, and
+  max * (1 / 127), its reciprocal and the value times that are one IEEE operation each, which NumPy's fp32 does alike; then to the nearest, ties to even.  So are plain scales.
   The norm's factor: a thread adds up to 64 squares, then 6 steps over lanes and 15 over wavefronts: the sum is off by at most 86 e, its square root by half of that;
   mean, rsqrt (one unit = 2 e), and two roundings behind it: 43 + 1 + 2 + 2, bounded by 50 e.
-  The gate: z is off by at most 4 e |z| (three products and a sum), which exp carries over as 4 e |z|, its own error 2 e, 1 + exp and the reciprocal 1 and 2 e, two
-  products 2 e: (8 + 4 |z|) e relative; where z < 0 the quotient is small and the bound holds all the same.  Below 2^-120 |b| results may vanish.
+  The gate: gelu's z comes from two constants and five operations, each e, so that it is off by at most 7 e |z| (silu's z is exact), which exp carries over; exp's own error
+  2 e, 1 + exp, the quotient and the product with b 1 e each, and 3 e to spare: (8 + 7 |z|) e relative.  Below 2^-120 |b| results may vanish.
   The product: the sum is exact; it, the scales' product and the result's are rounded in fp32: 3 e, and then u."""
 import numpy as np
 import pytest
@@ -129,9 +128,10 @@ def _sides_are_left(*wholes):
 
 
 def _codes(v, most):
-    """rne(v * (127 / most)) of exact values: the product has at most 48 bits, which 64-bit floats hold."""
-    inv = np.where(most < 2.0 ** -100, np.float32(0), np.float32(127) / np.where(most == 0, 1, most).astype(np.float32)).astype(np.float32)
-    return np.rint(v * inv.astype(np.float64)[:, None])
+    """rne(v * (1 / scale)), scale = most * (1 / 127), of values that fp32 holds, in its steps."""
+    step = np.where(most == 0, 1, most).astype(np.float32) * (np.float32(1) / np.float32(127))
+    inv = np.where(most < 2.0 ** -100, np.float32(0), np.float32(1) / step).astype(np.float32)
+    return np.rint(v.astype(np.float32) * inv[:, None])
 
 
 def _f64(t):
@@ -159,7 +159,7 @@ def test_plain_rows_are_exact(rtn, K, dtype):
         v = _f64(x)
         most = np.abs(v).max(1)
         assert np.array_equal(q.cpu().numpy(), _codes(v, most))
-        assert np.array_equal(s.view(M).cpu().numpy(), most.astype(np.float32) / np.float32(127))
+        assert np.array_equal(s.view(M).cpu().numpy(), most.astype(np.float32) * (np.float32(1) / np.float32(127)))
         _sides_are_left(wq, ws)
         for to in TYPES:
             wo, o = _bordered(M, K, to)
@@ -241,7 +241,7 @@ def test_gated_rows(rtn, K, activation, dtype):
         z = a if activation == "silu" else a * np.sqrt(8 / np.pi) * (1 + 0.044715 * a * a)
         with np.errstate(over="ignore"):
             v = a / (1 + np.exp(-z)) * b
-        rel = (8 + 4 * np.abs(z)) * E
+        rel = (8 + 7 * np.abs(z)) * E
         wo, o = _bordered(M, K, dtype)
         rtn.rtn_gated_rows(x, activation, out=o)
         assert (np.abs(_f64(o) - v) <= (UNIT[dtype] + rel) * np.abs(v) + TINY[dtype] * (1 + np.abs(b))).all()
@@ -257,7 +257,7 @@ def test_gated_rows(rtn, K, activation, dtype):
         assert (q.cpu().numpy()[~some] == 0).all() and (s.cpu().numpy()[~some] == 0).all()
         step = (most / 127)[some, None]
         far = np.abs(q.cpu().numpy()[some] - v[some] / step)
-        assert (far <= 0.5 + 2 * off[some, None] / step + 127 * 3 * E).all()
+        assert (far <= 0.5 + 2 * off[some, None] / step + 127 * 4 * E).all()
 
 
 @pytest.mark.gpu
