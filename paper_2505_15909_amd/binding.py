@@ -144,7 +144,8 @@ def _load_native():
         warnings.warn(f"the binding's native calls were compiled for {built_for}, this is {here}: build the library again", RuntimeWarning)
         return None
     module.bind(*(C.cast(f, C.c_void_p).value for f in (_lib.rtn_linear, _lib.rtn_linear_asym, _lib.rtn_cache_plan, _lib.rtn_rope_cache,
-                                                        _lib.rtn_paged_attention)))
+                                                        _lib.rtn_paged_attention, _lib.rtn_norm_rows, _lib.rtn_gated_rows, _lib.rtn_quantize_rows,
+                                                        _lib.rtn_dequantize_rows, _lib.rtn_linear_w8a8)))
     return module
 
 
@@ -672,6 +673,11 @@ def rtn_norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor 
                   residual_out: torch.Tensor = None, out=None):
     """x [rows, dim] (+ residual, the sum of which goes to residual_out, or back to residual) -> its root-mean-square norm times weight, in x's type,
     or quantised: (int8 [rows, dim], fp32 scales [rows])."""
+    if _native is not None and out is not None:
+        st = _native.norm_rows(x, weight, residual, eps, quantize, residual_out, out)
+        if st is not None:
+            _check(st, "rtn_norm_rows")
+            return out
     _dev_rows(x, "x")
     M, K = x.shape
     _dev_whole(weight, "weight", (K,), x.dtype)
@@ -692,6 +698,11 @@ def rtn_norm_rows(x: torch.Tensor, weight: torch.Tensor, residual: torch.Tensor 
 def rtn_gated_rows(x: torch.Tensor, activation: str = "silu", quantize: bool = False, out=None):
     """x [rows, 2 dim], gate and up side by side as their projection gives them -> act(gate) * up in x's type, or quantised as rtn_norm_rows gives it.
     activation: "silu" or "gelu_tanh"."""
+    if _native is not None and out is not None:
+        st = _native.gated_rows(x, ACTIVATION.get(activation), quantize, out)
+        if st is not None:
+            _check(st, "rtn_gated_rows")
+            return out
     _dev_rows(x, "x")
     M, K = x.shape[0], x.shape[1] // 2
     if x.shape[1] != 2 * K:
@@ -705,6 +716,11 @@ def rtn_gated_rows(x: torch.Tensor, activation: str = "silu", quantize: bool = F
 
 def rtn_quantize_rows(x: torch.Tensor, out=None):
     """x [rows, dim] -> (int8 [rows, dim], fp32 scales [rows])."""
+    if _native is not None and out is not None:
+        st = _native.quantize_rows(x, out)
+        if st is not None:
+            _check(st, "rtn_quantize_rows")
+            return out
     _dev_rows(x, "x")
     M, K = x.shape
     out, to = _row_outputs(M, K, x.dtype, True, out, x.device)
@@ -714,6 +730,11 @@ def rtn_quantize_rows(x: torch.Tensor, out=None):
 
 def rtn_dequantize_rows(q: torch.Tensor, q_scales: torch.Tensor, dtype: torch.dtype = torch.float16, out: torch.Tensor = None) -> torch.Tensor:
     """The values that quantised rows stand for, in `dtype` (or out's)."""
+    if _native is not None and out is not None:
+        st = _native.dequantize_rows(q, q_scales, out)
+        if st is not None:
+            _check(st, "rtn_dequantize_rows")
+            return out
     dtype = dtype if out is None else out.dtype
     if q.dim() != 2 or dtype not in _TYPES:
         raise ValueError("q must be a matrix, and its values fp16 or bf16")
@@ -734,6 +755,11 @@ def rtn_linear_w8a8_workspace_nbytes(M: int, N: int, K: int) -> int:
 def rtn_linear_w8a8(q: torch.Tensor, q_scales: torch.Tensor, qweight: torch.Tensor, scales: torch.Tensor, dtype: torch.dtype = torch.float16,
                     out: torch.Tensor = None, workspace: torch.Tensor = None) -> torch.Tensor:
     """Quantised rows int8 [M, K] with fp32 scales [M] times rtn_quantize(W, 8, 0)'s qweight and fp16 scales [N, 1] -> [M, N] in `dtype` (or out's)."""
+    if _native is not None and out is not None and workspace is not None:
+        st = _native.linear_w8a8(q, q_scales, qweight, scales, out, workspace)
+        if st is not None:
+            _check(st, "rtn_linear_w8a8")
+            return out
     dtype = dtype if out is None else out.dtype
     if q.dim() != 2 or dtype not in _TYPES:
         raise ValueError("q must be a matrix, and the result fp16 or bf16")

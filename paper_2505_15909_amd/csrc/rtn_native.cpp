@@ -5,6 +5,7 @@
 // and raises what there is to raise.
 #include <Python.h>
 #include <ATen/core/Tensor.h>
+#include <c10/hip/HIPFunctions.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 #include <algorithm>
@@ -19,6 +20,11 @@ decltype(&rtn_linear_asym) asym_fn = nullptr;
 decltype(&rtn_cache_plan) plan_fn = nullptr;
 decltype(&rtn_rope_cache) rope_fn = nullptr;
 decltype(&rtn_paged_attention) attend_fn = nullptr;
+decltype(&rtn_norm_rows) norm_fn = nullptr;
+decltype(&rtn_gated_rows) gated_fn = nullptr;
+decltype(&rtn_quantize_rows) quantize_fn = nullptr;
+decltype(&rtn_dequantize_rows) dequantize_fn = nullptr;
+decltype(&rtn_linear_w8a8) w8a8_fn = nullptr;
 
 bool plain(PyObject* o) {
     return Py_TYPE(o) == reinterpret_cast<PyTypeObject*>(THPVariableClass) || Py_TYPE(o) == reinterpret_cast<PyTypeObject*>(ParameterClass);
@@ -230,14 +236,191 @@ PyObject* paged_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
     return PyLong_FromLong((long)st);
 }
 
-// bind(rtn_linear, rtn_linear_asym, rtn_cache_plan, rtn_rope_cache, rtn_paged_attention): their addresses in the loaded library
+// ---- The 8-bit layer's calls, the same way.
+
+const at::Tensor* here(PyObject* o, at::ScalarType type, int64_t dim) {      // a plain tensor of this type on the current device
+    if (!plain(o)) return nullptr;
+    const at::Tensor& t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.scalar_type() == type && t.dim() == dim && t.device().index() == c10::hip::current_device() ? &t : nullptr;
+}
+
+bool row_type(PyObject* o, at::ScalarType* type, int* dtype) {
+    if (!plain(o)) return false;
+    *type = THPVariable_Unpack(o).scalar_type();
+    *dtype = *type == at::kHalf ? RTN_TYPE_F16 : RTN_TYPE_BF16;
+    return *type == at::kHalf || *type == at::kBFloat16;
+}
+
+struct Rows {
+    void* data = nullptr;
+    int64_t rows = 0, dim = 0, stride = 0;
+};
+
+bool rows_of(PyObject* o, at::ScalarType type, Rows* r) {      // a matrix with contiguous rows
+    const at::Tensor* const t = here(o, type, 2);
+    if (!t || (t->stride(1) != 1 && t->size(1) != 1)) return false;
+    *r = {t->data_ptr(), t->size(0), t->size(1), t->size(0) > 1 ? t->stride(0) : t->size(1)};
+    return true;
+}
+
+bool rows_like(PyObject* o, at::ScalarType type, int64_t rows, int64_t dim, Rows* r) { return rows_of(o, type, r) && r->rows == rows && r->dim == dim; }
+
+bool matrix(PyObject* o, at::ScalarType type, int64_t rows, int64_t dim, void** data) {      // contiguous
+    const at::Tensor* const t = here(o, type, 2);
+    if (!t || !t->is_contiguous() || (rows >= 0 && t->size(0) != rows) || (dim >= 0 && t->size(1) != dim)) return false;
+    *data = t->data_ptr();
+    return true;
+}
+
+bool vector(PyObject* o, at::ScalarType type, int64_t n, void** data) {
+    const at::Tensor* const t = here(o, type, 1);
+    if (!t || !t->is_contiguous() || t->size(0) != n) return false;
+    *data = t->data_ptr();
+    return true;
+}
+
+struct RowOutputs {
+    void *out16 = nullptr, *codes = nullptr, *scales = nullptr;
+};
+
+bool row_outputs(PyObject* quantize, PyObject* out, at::ScalarType type, int64_t rows, int64_t dim, RowOutputs* r) {
+    if (quantize == Py_False) return matrix(out, type, rows, dim, &r->out16);
+    return quantize == Py_True && PyTuple_CheckExact(out) && PyTuple_GET_SIZE(out) == 2 &&
+           matrix(PyTuple_GET_ITEM(out, 0), at::kChar, rows, dim, &r->codes) && vector(PyTuple_GET_ITEM(out, 1), at::kFloat, rows, &r->scales);
+}
+
+// (x, weight, residual, eps, quantize, residual_out, out) -> status, or None
+PyObject* norm_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int dtype;
+    Rows x, add, sum;
+    RowOutputs to;
+    void *weight, *stream;
+    try {
+        if (n != 7 || !norm_fn || !PyFloat_CheckExact(a[3]) || !row_type(a[0], &type, &dtype) || !rows_of(a[0], type, &x) ||
+            !vector(a[1], type, x.dim, &weight) || !row_outputs(a[4], a[6], type, x.rows, x.dim, &to))
+            Py_RETURN_NONE;
+        if (a[2] != Py_None) {
+            if (!rows_like(a[2], type, x.rows, x.dim, &add) || !rows_like(a[5] == Py_None ? a[2] : a[5], type, x.rows, x.dim, &sum)) Py_RETURN_NONE;
+        } else if (a[5] != Py_None) {
+            Py_RETURN_NONE;
+        }
+        stream = current_stream();
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    const float eps = (float)PyFloat_AS_DOUBLE(a[3]);
+    rtn_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = norm_fn(x.data, x.rows, x.stride, x.dim, dtype, add.data, add.stride, sum.data, sum.stride, weight, eps, to.out16, to.codes,
+                 static_cast<float*>(to.scales), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)st);
+}
+
+// (x, activation, quantize, out) -> status, or None; the activation as the C entry's number
+PyObject* gated_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int dtype;
+    Rows x;
+    RowOutputs to;
+    long activation;
+    void* stream;
+    try {
+        if (n != 4 || !gated_fn || !whole(a[1], &activation) || !row_type(a[0], &type, &dtype) || !rows_of(a[0], type, &x) || x.dim % 2 ||
+            !row_outputs(a[2], a[3], type, x.rows, x.dim / 2, &to))
+            Py_RETURN_NONE;
+        stream = current_stream();
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    rtn_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = gated_fn(x.data, x.rows, x.stride, x.dim / 2, dtype, (int)activation, to.out16, to.codes, static_cast<float*>(to.scales), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)st);
+}
+
+// (x, out) -> status, or None
+PyObject* quantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int dtype;
+    Rows x;
+    RowOutputs to;
+    void* stream;
+    try {
+        if (n != 2 || !quantize_fn || !row_type(a[0], &type, &dtype) || !rows_of(a[0], type, &x) || !row_outputs(Py_True, a[1], type, x.rows, x.dim, &to)) Py_RETURN_NONE;
+        stream = current_stream();
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    rtn_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = quantize_fn(x.data, x.rows, x.stride, x.dim, dtype, to.codes, static_cast<float*>(to.scales), stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)st);
+}
+
+// (q, q_scales, out) -> status, or None
+PyObject* dequantize_rows(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int dtype;
+    Rows q;
+    void *scales, *out, *stream;
+    try {
+        if (n != 3 || !dequantize_fn || !row_type(a[2], &type, &dtype) || !rows_of(a[0], at::kChar, &q) || !matrix(a[0], at::kChar, q.rows, q.dim, &q.data) ||
+            !vector(a[1], at::kFloat, q.rows, &scales) || !matrix(a[2], type, q.rows, q.dim, &out))
+            Py_RETURN_NONE;
+        stream = current_stream();
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    rtn_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = dequantize_fn(q.data, static_cast<const float*>(scales), q.rows, q.dim, dtype, out, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)st);
+}
+
+// (q, q_scales, qweight, scales, out, workspace) -> status, or None
+PyObject* linear_w8a8(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    at::ScalarType type;
+    int dtype;
+    int64_t M, N, K;
+    void *q, *qs, *w, *s, *out, *ws, *stream;
+    size_t bytes;
+    try {
+        if (n != 6 || !w8a8_fn || !row_type(a[4], &type, &dtype)) Py_RETURN_NONE;
+        const at::Tensor *const x = here(a[0], at::kChar, 2), *const scales = here(a[3], at::kHalf, 2);
+        if (!x || !scales || !plain(a[5])) Py_RETURN_NONE;
+        M = x->size(0); K = x->size(1); N = scales->size(0);
+        const at::Tensor& work = THPVariable_Unpack(a[5]);
+        if (N < 1 || N > INT64_MAX / std::max<int64_t>(K, 1) || !matrix(a[0], at::kChar, M, K, &q) || !matrix(a[3], at::kHalf, N, 1, &s) ||
+            !vector(a[1], at::kFloat, M, &qs) || !vector(a[2], at::kByte, N * K, &w) || !matrix(a[4], type, M, N, &out) || !work.is_cuda() || !work.is_contiguous() ||
+            work.device() != x->device())
+            Py_RETURN_NONE;
+        ws = work.data_ptr();
+        bytes = work.nbytes();
+        stream = current_stream();
+    } catch (...) {
+        Py_RETURN_NONE;
+    }
+    rtn_status st;
+    Py_BEGIN_ALLOW_THREADS
+    st = w8a8_fn(q, static_cast<const float*>(qs), M, w, s, N, K, dtype, out, ws, bytes, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong((long)st);
+}
+
+// bind(rtn_linear, rtn_linear_asym, rtn_cache_plan, rtn_rope_cache, rtn_paged_attention, rtn_norm_rows, rtn_gated_rows, rtn_quantize_rows,
+// rtn_dequantize_rows, rtn_linear_w8a8): their addresses in the loaded library
 PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
-    if (n != 5) {
-        PyErr_SetString(PyExc_TypeError, "bind takes five addresses");
+    if (n != 10) {
+        PyErr_SetString(PyExc_TypeError, "bind takes ten addresses");
         return nullptr;
     }
-    void* f[5];
-    for (int i = 0; i < 5; ++i) {
+    void* f[10];
+    for (int i = 0; i < 10; ++i) {
         f[i] = PyLong_AsVoidPtr(args[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -246,6 +429,11 @@ PyObject* bind(PyObject*, PyObject* const* args, Py_ssize_t n) {
     plan_fn = reinterpret_cast<decltype(plan_fn)>(f[2]);
     rope_fn = reinterpret_cast<decltype(rope_fn)>(f[3]);
     attend_fn = reinterpret_cast<decltype(attend_fn)>(f[4]);
+    norm_fn = reinterpret_cast<decltype(norm_fn)>(f[5]);
+    gated_fn = reinterpret_cast<decltype(gated_fn)>(f[6]);
+    quantize_fn = reinterpret_cast<decltype(quantize_fn)>(f[7]);
+    dequantize_fn = reinterpret_cast<decltype(dequantize_fn)>(f[8]);
+    w8a8_fn = reinterpret_cast<decltype(w8a8_fn)>(f[9]);
     Py_RETURN_NONE;
 }
 
@@ -255,6 +443,11 @@ PyMethodDef methods[] = {
     {"cache_plan", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(cache_plan)), METH_FASTCALL, nullptr},
     {"rope_cache", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(rope_cache)), METH_FASTCALL, nullptr},
     {"paged_attention", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(paged_attention)), METH_FASTCALL, nullptr},
+    {"norm_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(norm_rows)), METH_FASTCALL, nullptr},
+    {"gated_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(gated_rows)), METH_FASTCALL, nullptr},
+    {"quantize_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(quantize_rows)), METH_FASTCALL, nullptr},
+    {"dequantize_rows", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(dequantize_rows)), METH_FASTCALL, nullptr},
+    {"linear_w8a8", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(linear_w8a8)), METH_FASTCALL, nullptr},
     {"bind", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(bind)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 

@@ -107,6 +107,18 @@ def test_binding_refuses_what_is_not_on_the_gpu():
             call()
 
 
+def test_native_calls_leave_what_they_do_not_take():
+    from paper_2505_15909_amd import binding
+    x, w = torch.zeros(2, 64, dtype=torch.float16), torch.zeros(64, dtype=torch.float16)
+    q, s = torch.zeros(2, 64, dtype=torch.int8), torch.zeros(2)
+    for call, args in ((binding._native.norm_rows, (x, w, None, 1e-6, False, None, x)), (binding._native.gated_rows, (x, 0, False, x[:, :32])),
+                       (binding._native.quantize_rows, (x, (q, s))), (binding._native.dequantize_rows, (q, s, x)),
+                       (binding._native.linear_w8a8, (q, s, q.view(torch.uint8).view(-1), x[:, :1], x, x))):
+        assert call(*args) is None                           # (nothing of it is on a GPU)
+        assert call(*args[:-1]) is None
+        assert call(*[None] * len(args)) is None
+
+
 # ---- rows ---------------------------------------------------------------------------------------------------------------------------
 
 def _matrix(M, K, pad, dtype, seed, scale=1.0):
@@ -514,3 +526,52 @@ def test_binding_checks(rtn):
         rtn.rtn_quantize_rows(torch.randn(4, 516, device=DEV).half()[:, :512])           # rows that begin between two pieces
     one = torch.randn(1, 516, device=DEV).half()[:, :512]    # of one row, the stride says nothing
     assert torch.equal(rtn.rtn_quantize_rows(one)[0], rtn.rtn_quantize_rows(one.clone())[0])
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", TYPES)
+def test_native_calls_and_python_give_the_same(rtn, dtype, monkeypatch):
+    """With outputs given a call is read in native code: the same results, and the same refusals from the Python code that it leaves them to."""
+    from paper_2505_15909_amd import binding
+    x, r, w = _matrix(5, 512, 8, dtype, 1), _matrix(5, 512, 0, dtype, 2), _matrix(1, 512, 0, dtype, 3)[0]
+    W = torch.randn(64, 512, device=DEV).half()
+    qw = rtn.rtn_quantize(W, 8, 0)
+    work = torch.empty(1 << 20, dtype=torch.uint8, device=DEV)
+
+    def calls(out, half, codes, sums):
+        yield rtn.rtn_norm_rows(x, w, out=out), out
+        yield rtn.rtn_norm_rows(x, w, residual=r, residual_out=sums, quantize=True, out=codes), codes
+        yield rtn.rtn_quantize_rows(x, out=codes), codes
+        yield rtn.rtn_dequantize_rows(*codes, out=out), out
+        yield rtn.rtn_linear_w8a8(*codes, *qw, out=half[:, :64].contiguous(), workspace=work), None
+        yield rtn.rtn_gated_rows(x, "gelu_tanh", out=half), half
+        short = codes[0][:, :256].contiguous(), codes[1]
+        yield rtn.rtn_gated_rows(x, quantize=True, out=short), short
+
+    def results():
+        buffers = torch.empty(5, 512, dtype=dtype, device=DEV), torch.empty(5, 256, dtype=dtype, device=DEV), \
+            (torch.empty(5, 512, dtype=torch.int8, device=DEV), torch.empty(5, device=DEV)), torch.empty(5, 512, dtype=dtype, device=DEV)
+        got = []
+        for y, given in calls(*buffers):
+            assert given is None or y is given or all(a is b for a, b in zip(y, given))
+            got += [t.clone() for t in (y if isinstance(y, tuple) else (y,))]
+        return got + [buffers[3].clone()]
+
+    native = results()
+    taken = []
+    for name in ("norm_rows", "gated_rows", "quantize_rows", "dequantize_rows", "linear_w8a8"):
+        call = getattr(binding._native, name)
+        monkeypatch.setattr(binding._native, name, lambda *a, call=call: taken.append(call(*a)) or taken[-1])
+    again = results()
+    assert taken == [0] * 7
+    monkeypatch.setattr(binding, "_native", None)
+    python = results()
+    for a, b, c in zip(native, again, python):
+        assert torch.equal(a, b) and torch.equal(a, c)
+    half = torch.empty(5, 256, dtype=dtype, device=DEV)
+    monkeypatch.undo()
+    for call in (lambda: rtn.rtn_norm_rows(x, w, out=half), lambda: rtn.rtn_norm_rows(x, w.float(), out=torch.empty_like(r)), lambda: rtn.rtn_gated_rows(x, "relu", out=half),
+                 lambda: rtn.rtn_gated_rows(x[:, :511], out=half), lambda: rtn.rtn_quantize_rows(x, out=(half, half)),
+                 lambda: rtn.rtn_norm_rows(x, w, residual_out=r, out=torch.empty_like(r))):
+        with pytest.raises(ValueError):
+            call()
