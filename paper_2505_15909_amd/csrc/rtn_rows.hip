@@ -7,7 +7,8 @@
 // h w is exact in fp32 (two significands of at most 11 bits); every other step is one rounding in fp32, in the order that the header of the entry points
 // gives, so that the codes of plain and normed rows are what the same steps give anywhere else.
 //
-// Bound by memory: the norm with a residual moves 7 bytes an element quantised, the gated activation 5, plain rows 3.
+// Bound by memory: the norm with a residual moves 7 bytes an element quantised, the gated activation 5, plain rows 3 (8192 x 8192 in 82 us,
+// 5.7 TB/s; 4096 x 28672 in 107 us, 5.5; 3001 x 16384 in 27.7, 5.3, where a copy of 1 GiB reaches 4.8 to 5.5).
 #include "rtn_paged.h"
 
 namespace rtn {
@@ -74,6 +75,12 @@ __device__ __forceinline__ uint32_t four_codes(const float* v, float inv) {
     return __builtin_amdgcn_perm(__builtin_amdgcn_perm(t[3], t[2], 0x0C0C0400u), __builtin_amdgcn_perm(t[1], t[0], 0x0C0C0400u), 0x05040100u);
 }
 
+// 16-bit results, sums and the values of codes are stored as streaming: 8192 x 8192 normed and then dequantised 126 -> 112 us, 4096 x 28672 gated
+// and dequantised 193 -> 172, 1897 x 5120 normed 7.7 -> 7.0.  Codes are not: they are few, and what reads them next finds them in the caches (3001 x 16384 quantised and
+// dequantised 51, as streaming 55).  Streaming loads gained nothing in such pairs.
+template <typename V>
+__device__ __forceinline__ void store_out(void* at, V v) { __builtin_nontemporal_store(v, static_cast<V*>(at)); }
+
 // T threads a row, C pieces of eight elements a thread; workgroups of at least 256 threads.
 template <int TYPE, int OP, bool QUANT, int T, int C>
 __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams p) {
@@ -115,7 +122,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams
                 // the sum is held in the type, as the next layer finds it, and what is held is normed
 #pragma unroll
                 for (int i = 0; i < 8; ++i) in[c][i] = (E)((float)in[c][i] + (float)with[c][i]);
-                *reinterpret_cast<E8*>(static_cast<E*>(p.sum) + row * p.sum_stride + k) = in[c];
+                store_out(static_cast<E*>(p.sum) + row * p.sum_stride + k, in[c]);
             }
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -167,7 +174,7 @@ __global__ __launch_bounds__(T < 256 ? 256 : T) void rows_kernel(const RowParams
             E8 y;
 #pragma unroll
             for (int i = 0; i < 8; ++i) y[i] = (E)(value(c, i) * factor);
-            *reinterpret_cast<E8*>(static_cast<E*>(p.out) + (int64_t)row * p.dim + k) = y;
+            store_out(static_cast<E*>(p.out) + (int64_t)row * p.dim + k, y);
         }
     }
 }
@@ -188,7 +195,7 @@ __global__ __launch_bounds__(256) void dequantize_rows_kernel(const uint8_t* q, 
         E8 y;
 #pragma unroll
         for (int i = 0; i < 8; ++i) y[i] = (E)((float)(int8_t)(codes[i / 4] >> (i % 4 * 8)) * s);
-        *reinterpret_cast<E8*>(static_cast<E*>(out) + at + k) = y;
+        store_out(static_cast<E*>(out) + at + k, y);
     }
 }
 
@@ -200,11 +207,14 @@ static void launch_rows_as(const RowParams& p, hipStream_t st) {
 
 template <int TYPE, int OP, bool QUANT>
 static hipError_t launch_rows(const RowParams& p, hipStream_t st) {
+    // About as many threads as a row has pieces, so that a few rows do not wait (256 rows of 8192 normed: 1024 threads 4.6 us, 512 4.7, 256 5.4; 64 of 16384 5.0,
+    // 5.3, 7.1), and two to four pieces each once there are many (8192 rows of 8192: 83.2, 81.7, 83.5).
     const int pieces = p.dim / 8;
     if (pieces <= 64) launch_rows_as<TYPE, OP, QUANT, 64, 1>(p, st);
     else if (pieces <= 256) launch_rows_as<TYPE, OP, QUANT, 256, 1>(p, st);
     else if (pieces <= 512) launch_rows_as<TYPE, OP, QUANT, 256, 2>(p, st);
-    else if (pieces <= 1024) launch_rows_as<TYPE, OP, QUANT, 256, 4>(p, st);
+    else if (pieces <= 768) launch_rows_as<TYPE, OP, QUANT, 256, 3>(p, st);
+    else if (pieces <= 1024) launch_rows_as<TYPE, OP, QUANT, 512, 2>(p, st);
     else if (pieces <= 2048) launch_rows_as<TYPE, OP, QUANT, 1024, 2>(p, st);
     else if (pieces <= 4096) launch_rows_as<TYPE, OP, QUANT, 1024, 4>(p, st);
     else launch_rows_as<TYPE, OP, QUANT, 1024, 8>(p, st);
