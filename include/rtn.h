@@ -433,8 +433,8 @@ rtn_status rtn_dequantize_rows(const void* dev_q, const float* dev_q_scales, int
  *   dev_C          out  [M, N] in `dtype`, RTN_TYPE_F16 or RTN_TYPE_BF16
  *   dev_workspace  scratch for the partial sums of K splits, rtn_linear_w8a8_workspace_nbytes() bytes (at most 64 MiB); with less or NULL K is split less
  *                  (slower, not an error); contents undefined before and after; calls that overlap in time need distinct ones
- * N % 16 == 0, K % 256 == 0, K < 2^17 (so that no sum leaves 32 bits), N * K below 0x7FFF0000, M 0 .. 2^20 (0: nothing to do), N <= 2^30.  The sums being exact, a
- * call gives the same bits whatever its workspace. */
+ * N % 16 == 0, K % 256 == 0, K < 2^17 (so that no sum leaves 32 bits), N * K below 0x7FFF0000, M 0 .. 2^20 (0: nothing to do), and no more tiles of results than a launch has
+ * threads for (M N up to 2^37 always fits; RTN_ERR_SHAPE where they do not).  The sums being exact, a call gives the same bits whatever its workspace. */
 size_t rtn_linear_w8a8_workspace_nbytes(int64_t M, int64_t N, int64_t K);
 rtn_status rtn_linear_w8a8(const void* dev_q, const float* dev_q_scales, int64_t M, const void* dev_qweight, const void* dev_scales, int64_t N, int64_t K,
                            int dtype, void* dev_C, void* dev_workspace, size_t workspace_nbytes, void* stream);

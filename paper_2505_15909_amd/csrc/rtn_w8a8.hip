@@ -32,6 +32,16 @@ __device__ __forceinline__ u32x2_t four_results(int4_t sum, float row_scale, hal
     return __builtin_bit_cast(u32x2_t, y);
 }
 
+// Workgroups on other columns read the same activations, and with K a power of two their weights start on the same memory channels.  Each begins at another place of
+// its n steps along K and goes round (sums of whole numbers have no order).  16 rows of 28672 x 4096 26.0 -> 20.9 us, 64 rows 26.2 -> 22.0; 16 rows of 28672 x
+// 8192 41.3 -> 37.7; where K is no power of two the same to 3 % (K = 4352: 21.5 and 22.6).  Tiles, whose neighbours take turns on an L2's contents, are 2 % slower that way.
+__device__ __forceinline__ int first_step(int column_tile, int n) { return (int)__umulhi((uint32_t)column_tile * 2654435769u, (uint32_t)n); }
+__device__ __forceinline__ int around(int i, int n) { return i < n ? i : i - n; }
+
+// The 16-byte piece of a row's 128 columns that stands at place v of eight: place kq (+ 4) is the piece that weight_operand's lane kq multiplies.  A row's places are
+// stored at v ^ (row & 7), and in this order the lanes that LDS serves together are on different banks.
+__device__ __forceinline__ int piece_at(int v) { return (v & 4) | (v & 1) << 1 | (v >> 1 & 1); }
+
 struct W8A8Params {
     const int8_t* A;
     const float* a_scales;
@@ -61,6 +71,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
     const int x = b / p.YB, y = b - x * p.YB;
     const int t0 = (int)((int64_t)p.KT * z / p.split), t1 = (int)((int64_t)p.KT * (z + 1) / p.split);
     const int n = max(0, (t1 - t0 - wave + WK - 1) / WK);    // this wavefront's tiles: t0 + wave + WK i
+    const int begin = first_step(x, n);
 
     // Through resources that start at this workgroup's rows: rows past M or N read zeros, at no cost.
     const int m0 = y * (16 * MB), K = p.KT * 64, a_rows = min(16 * MB, p.M - m0), b_tiles = min(NT, p.N / 16 - x * NT);
@@ -70,7 +81,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
     uint32_t a_at[MB], b_at[NT];
 #pragma unroll
     for (int i = 0; i < MB; ++i)
-        a_at[i] = 16 * i + nl < a_rows ? (uint32_t)(16 * i + nl) * (uint32_t)K + ((kq & 1) * 2 + (kq >> 1)) * 16 : kNoRow;
+        a_at[i] = 16 * i + nl < a_rows ? (uint32_t)(16 * i + nl) * (uint32_t)K + piece_at(kq) * 16 : kNoRow;
 #pragma unroll
     for (int j = 0; j < NT; ++j) b_at[j] = j < b_tiles ? (uint32_t)j * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
 
@@ -82,7 +93,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
     int4_t a[D][MB];
     u32x4_t w[D][NT];
     auto load = [&](int s, int i) {
-        const int t = t0 + wave + WK * min(i, n - 1);
+        const int t = t0 + wave + WK * around(begin + min(i, n - 1), n);
 #pragma unroll
         for (int j = 0; j < NT; ++j) w[s][j] = __builtin_amdgcn_raw_buffer_load_b128(rb, b_at[j], t * 1024, kStreaming);
 #pragma unroll
@@ -140,7 +151,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
 
 // ---- Many rows: bound by the matrix cores, at the clock that the power allows.  A workgroup of 8 wavefronts (2 along M x 4 along N) computes
 // 32 MBW rows x 256 columns of C, a wavefront 16 MBW x 64 of them.  K advances by 128 columns a step: 128 bytes of a row are eight 16-byte pieces in
-// LDS, piece p at slot p ^ (row & 7) (conflict-free both ways); packed tiles lie as they are, a lane reads its own chunk.  Both come
+// LDS (piece_at); packed tiles lie as they are, a lane reads its own chunk.  Both come
 // straight into LDS, SA and SB steps ahead.  A step runs in phases of two row blocks and both halves of its columns; a phase reads the next one's operands, and
 // the one barrier of a step stands before its last phase, whose operands are in registers by then: the stage is free behind it, and the
 // requests for it go out over the phases that follow. ----
@@ -186,7 +197,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
     const __amdgpu_buffer_rsrc_t rb =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(p.B) + (int64_t)(n0 / 16) * p.KT * 1024, 0, (uint32_t)b_tiles * (uint32_t)p.KT * 1024u, kBufferFlags);
     uint32_t a_lane[NA], b_lane[NB / 2];
-    const int st_row = lane >> 3, st_piece = (lane & 7) ^ (lane >> 3);
+    const int st_row = lane >> 3, st_piece = piece_at((lane & 7) ^ (lane >> 3));
 #pragma unroll
     for (int i = 0; i < NA; ++i) {
         const int row = (wave * NA + i) * 8 + st_row;
@@ -208,8 +219,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
 #pragma unroll
         for (int r = 0; r < 4; ++r) acc[b][r] = (int4_t){0, 0, 0, 0};
     const uint32_t a_rd = (uint32_t)((wm * (TM / 2) + nl) * 128), b_rd = (uint32_t)(wn * 8192 + lane * 16);
-    const int sixteen = (kq & 1) * 2 + (kq >> 1);            // the columns that weight_operand gives this lane
-    const uint32_t po0 = (uint32_t)((sixteen ^ (nl & 7)) * 16), po1 = (uint32_t)(((4 + sixteen) ^ (nl & 7)) * 16);
+    const uint32_t po0 = (uint32_t)((kq ^ (nl & 7)) * 16), po1 = (uint32_t)(((4 + kq) ^ (nl & 7)) * 16);
     int4_t aop[2][2][2];                                     // of two phases, row block, half
     int4_t bop[2][4];                                        // half, tile row
     u32x4_t raw[2][4];
@@ -352,8 +362,10 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
 // ---- Rows between: bound by the stream of weights where enough of them is on its way.  The eight wavefronts of a workgroup stand 8 / WK along N and WK along K.
 // A wavefront has NT tile rows of weights, straight into registers; the activations, 16 MB rows, come into LDS once for the wavefronts along N.
 // A step is 128 columns for each wavefront along K; both are requested S - 1 steps ahead, and one barrier a step says that its activations have landed
-// and the last one's are used up.  The wavefronts along K add up in LDS at the end. ----
-template <int TYPE, int MB, int NT, int WK, int S>
+// and the last one's are used up.  The wavefronts along K add up in LDS at the end.  ONCE: the weights are marked as read once -- one row tile, or more weights
+// than the L2s hold: 64 rows of 8192 x 28672 43.9 us, 46.8 unmarked; marked where two row tiles share them, 128 rows of 4096 x 4096 take 9.6 for 8.3,
+// 160 of 5120 x 5120 14.0 for 12.0. ----
+template <int TYPE, int MB, int NT, int WK, int S, bool ONCE>
 __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) void w8a8_block_kernel(const W8A8Params p) {
     constexpr int WN = 8 / WK, NA = MB * WK / 4, EACH = NA + 2 * NT;         // requests of a wavefront and step: of activations, in all
     constexpr int A_BYTES = MB * WK * 2048;
@@ -367,7 +379,7 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
     if (!xcd_tile((int)blockIdx.x - z * blocks, p.XB, p.YB, kZGroup, &xb, &yb)) return;
     const int m0 = yb * (16 * MB), K = p.KT * 64, tile0 = (xb * WN + wn) * NT;
     const int s0 = (int)((int64_t)(p.KT / 2) * z / p.split), units = (int)((int64_t)(p.KT / 2) * (z + 1) / p.split) - s0;      // of 128 columns
-    const int T = (units + WK - 1) / WK;
+    const int T = (units + WK - 1) / WK, begin = first_step(xb, units);
 
     const int a_rows = min(16 * MB, p.M - m0), b_tiles = __builtin_amdgcn_readfirstlane(max(0, min(NT, p.N / 16 - tile0)));      // (none: a wavefront beyond N)
     const int first = __builtin_amdgcn_readfirstlane(min(tile0, p.N / 16 - 1));
@@ -380,7 +392,7 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
     for (int i = 0; i < NA; ++i) {
         const int r = wave * NA + i, row = r % (2 * MB) * 8 + (lane >> 3);
         a_unit[i] = r / (2 * MB);
-        a_lane[i] = row < a_rows ? (uint32_t)row * (uint32_t)K + ((lane & 7) ^ (lane >> 3)) * 16 : kNoRow;
+        a_lane[i] = row < a_rows ? (uint32_t)row * (uint32_t)K + piece_at((lane & 7) ^ (lane >> 3)) * 16 : kNoRow;
     }
 #pragma unroll
     for (int j = 0; j < NT; ++j) b_lane[j] = j < b_tiles ? (uint32_t)j * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
@@ -388,12 +400,12 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
     u32x4_t w[S][NT][2];
     auto request = [&](int u, int t) {                       // step t, into stage and registers u; units past the last one: the last, not multiplied
 #pragma unroll
-        for (int i = 0; i < NA; ++i) load_to_lds(ra, stage(u) + (wave * NA + i) * 1024, a_lane[i], (s0 + min(t * WK + a_unit[i], units - 1)) * 128);
-        const int at = s0 + min(t * WK + wk, units - 1);
+        for (int i = 0; i < NA; ++i) load_to_lds(ra, stage(u) + (wave * NA + i) * 1024, a_lane[i], (s0 + around(begin + min(t * WK + a_unit[i], units - 1), units)) * 128);
+        const int at = s0 + around(begin + min(t * WK + wk, units - 1), units);
 #pragma unroll
         for (int j = 0; j < NT; ++j)
 #pragma unroll
-            for (int h = 0; h < 2; ++h) w[u][j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, b_lane[j], at * 2048 + h * 1024, kStreaming);
+            for (int h = 0; h < 2; ++h) w[u][j][h] = __builtin_amdgcn_raw_buffer_load_b128(rb, b_lane[j], at * 2048 + h * 1024, ONCE ? kStreaming : 0);
         __builtin_amdgcn_sched_barrier(0);
     };
     int4_t acc[MB][NT];
@@ -401,8 +413,7 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
     for (int b = 0; b < MB; ++b)
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[b][j] = (int4_t){0, 0, 0, 0};
-    const int sixteen = (kq & 1) * 2 + (kq >> 1);
-    const uint32_t a_rd = (uint32_t)(wk * MB * 2048 + nl * 128), po[2] = {(uint32_t)((sixteen ^ (nl & 7)) * 16), (uint32_t)(((4 + sixteen) ^ (nl & 7)) * 16)};
+    const uint32_t a_rd = (uint32_t)(wk * MB * 2048 + nl * 128), po[2] = {(uint32_t)((kq ^ (nl & 7)) * 16), (uint32_t)(((4 + kq) ^ (nl & 7)) * 16)};
     auto step = [&](int u, int t) {
         __builtin_amdgcn_sched_barrier(0);
         wait_and_barrier<(S - 2) * EACH>();
@@ -488,21 +499,24 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 
 // The kernels' shapes and what their time is made of, in us.  Stream and block kernels: start + units x (workgroups on the fullest compute unit) x
 // (each + more x the share of a workgroup's rows that M has), a unit being the 64 (128) columns of a step of each wavefront along K: a compute unit
-// gets 50 to 65 GB/s out of the L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup a compute unit, whose step takes `each` where half
-// the chip is busy and `each + more` where all of it is (power).  That against the weights' stream, and a K split's join.  Fitted to 16 000 launches
-// over 900 problems (1 to 8192 rows, 256 to 57344 columns, K 1024 to 28672): 7 to 12 % rms, and the pick is 1.6 % behind the best of all launches on the mean.
+// has some 32 KiB on their way at once, 50 to 65 GB/s where they come from beyond its L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup
+// a compute unit, whose step takes `each` where half the chip is busy and `each + more` where all of it is (power).  That against the weights' stream,
+// and a K split's join.  Fitted to 20 000 launches over 750 problems (1 to 8192 rows, 256 to 57344 columns, K 1024 to 28672): 7 to 11 % rms (15 for
+// 64 rows with four wavefronts along K), and the pick is 1.8 % behind the best of all launches on the mean, 24 % at most.
 enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
 struct W8A8Shape {
     int kind, mb, nt, wk, depth;
     float start, each, more;
 };
 constexpr W8A8Shape kShapes[] = {
-    {W8A8_STREAM, 1, 1, 8, 4, 3.46f, 0.123f, 0.271f}, {W8A8_STREAM, 1, 1, 8, 2, 3.53f, 0.157f, 0.221f}, {W8A8_STREAM, 1, 2, 8, 2, 3.29f, 0.276f, 0.286f},
-    {W8A8_STREAM, 1, 4, 8, 2, 3.22f, 0.576f, 0.382f}, {W8A8_STREAM, 2, 2, 8, 2, 3.18f, 0.348f, 0.468f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.38f, 0.462f, 0.051f},
-    {W8A8_BLOCK, 2, 2, 4, 3, 3.54f, 0.831f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.06f, 0.699f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.54f, 0.519f, 0.283f},
-    {W8A8_BLOCK, 4, 1, 2, 3, 3.93f, 0.463f, 0.057f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.26f, 0.414f, 0.f},     {W8A8_BLOCK, 4, 2, 2, 3, 4.63f, 0.837f, 0.f},
-    {W8A8_BLOCK, 8, 2, 2, 3, 6.48f, 1.134f, 0.024f},  {W8A8_BLOCK, 8, 2, 1, 3, 6.58f, 0.917f, 0.f},     {W8A8_TILE, 4, 0, 0, 0, 6.17f, 0.724f, 0.170f},
-    {W8A8_TILE, 8, 0, 0, 0, 7.86f, 1.117f, 0.352f}};
+    {W8A8_STREAM, 1, 1, 8, 4, 3.38f, 0.129f, 0.219f}, {W8A8_STREAM, 1, 1, 8, 2, 3.33f, 0.179f, 0.159f}, {W8A8_STREAM, 1, 2, 8, 2, 3.16f, 0.294f, 0.236f},
+    {W8A8_STREAM, 1, 4, 8, 2, 3.09f, 0.625f, 0.244f}, {W8A8_STREAM, 2, 2, 8, 2, 3.00f, 0.399f, 0.392f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.36f, 0.479f, 0.059f},
+    {W8A8_BLOCK, 2, 2, 4, 3, 3.28f, 0.881f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 3.95f, 0.696f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.35f, 0.496f, 0.406f},
+    {W8A8_BLOCK, 4, 1, 2, 3, 3.98f, 0.436f, 0.129f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.42f, 0.364f, 0.104f},  {W8A8_BLOCK, 4, 2, 2, 3, 4.75f, 0.793f, 0.115f},
+    {W8A8_BLOCK, 4, 2, 1, 3, 5.11f, 0.715f, 0.051f},  {W8A8_BLOCK, 8, 2, 2, 3, 7.21f, 1.006f, 0.260f},  {W8A8_TILE, 4, 0, 0, 0, 5.60f, 0.719f, 0.186f},
+    {W8A8_TILE, 8, 0, 0, 0, 7.85f, 1.066f, 0.431f}};
+// Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
+constexpr float kSharedStream = 1.209f, kSharedNear = 0.706f, kSharedFar = 0.957f;
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 struct W8A8Plan {
@@ -523,13 +537,15 @@ template <int... I>
 constexpr std::array<W8A8Cover, sizeof...(I)> covers(std::integer_sequence<int, I...>) { return {cover_of(kShapes[I])...}; }
 constexpr auto kCovers = covers(std::make_integer_sequence<int, kShapeCount>());
 
-// (0.3 us for a few rows, 0.8 where most of the shapes are looked at.)
+// Weights that the L2s hold together: row tiles that share them find them there.
+static bool weights_near(int64_t N, int64_t K) { return N * K <= (int64_t)32 << 20; }
+
 static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
     W8A8Plan plan = {};
     float best = 1e30f;
     const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.12e6f);
     const float s4 = stream * stream * stream * stream;
-    const int splits = (int)std::min(8.f, (float)std::min(workspace, kW8A8Workspace) * 0.25f / MN);      // (below 8 in all where that is near)
+    const int splits = (int)std::min<uint64_t>(8, std::min(workspace, kW8A8Workspace) / 4 / (uint64_t)(M * N));
     const int pieces = (int)((M + 15) / 16);
     auto up = [](int64_t n, int log2) { return (n + ((int64_t)1 << log2) - 1) >> log2; };
     for (int i = 0; i < kShapeCount; ++i) {
@@ -538,8 +554,9 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
         if ((1 << c.rows) >= 32 * pieces && c.rows > 5) continue;            // mostly rows beyond M
         if (k.kind != W8A8_TILE && pieces > 8 << (c.rows - 4)) continue;     // the weights eight times and more
         const int64_t XB = up(N, c.columns), YB = up(M, c.rows), tiles = XB * YB, all_units = K >> c.unit;
-        const float unit_us = k.each + k.more * (float)M / (float)(YB << c.rows);
-        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 2.45e6f));
+        const float shared = YB == 1 ? 1.f : k.kind == W8A8_STREAM ? kSharedStream : weights_near(N, K) ? kSharedNear : kSharedFar;
+        const float unit_us = (k.each + k.more * (float)M / (float)(YB << c.rows)) * shared;
+        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 2.81e6f));
         for (int split = 1; split <= std::max(1, splits); ++split) {
             if (split > 1 && ((split << c.along) > all_units || tiles * split > 800)) break;
             const float steps = (float)up((uint32_t)(all_units + split - 1) / (uint32_t)split, c.along);
@@ -547,12 +564,12 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
             if (k.kind == W8A8_TILE) {
                 const int64_t on_xcd = up(tiles, 3) * split;
                 const float part = (float)(on_xcd & 31) * (1.f / 32.f);
-                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 5.3f) - 5.3f;
-                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 5.3f;
+                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 5.54f) - 5.54f;
+                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 5.54f;
             } else {
                 work = steps * unit_us * (float)(k.kind == W8A8_STREAM ? up(tiles * split, 8) : up(up(tiles, 3) * split, 5));
             }
-            const float rest = once + (split > 1 ? 2.84f + (outputs + 4.f * outputs * (float)split) * (1.f / 6.12e6f) : 0.f);
+            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 3.90f : 2.77f) + (outputs + 4.f * outputs * (float)split) * (1.f / 6.76e6f) : 0.f);
             if (rest + std::max(work, stream) >= best) continue;
             const float t = rest + std::sqrt(std::sqrt(work * work * work * work + s4));
             if (t < best) {
@@ -573,7 +590,10 @@ template <int TYPE, int I>
 static void launch_shape(const W8A8Params& p, dim3 grid, hipStream_t st) {
     constexpr W8A8Shape k = kShapes[I];
     if constexpr (k.kind == W8A8_STREAM) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, k.mb, k.nt, k.wk, k.depth>), grid, dim3(k.wk * 64), 0, st, p);
-    else if constexpr (k.kind == W8A8_BLOCK) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, k.depth>), grid, dim3(512), 0, st, p);
+    else if constexpr (k.kind == W8A8_BLOCK) {
+        if (p.YB == 1 || !weights_near(p.N, (int64_t)p.KT * 64)) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, k.depth, true>), grid, dim3(512), 0, st, p);
+        else hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, k.depth, false>), grid, dim3(512), 0, st, p);
+    }
     else hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, k.mb>), grid, dim3(kTileThreads), 0, st, p);
 }
 

@@ -81,7 +81,7 @@ def test_dequantize_refusals(kw, status):
 
 @pytest.mark.parametrize("kw,status", [({"M": 1, "q": None}, NULL), ({"M": 1, "s": None}, NULL), ({"M": 1, "w": None}, NULL), ({"M": 1, "ws": None}, NULL), ({"M": 1, "C": None}, NULL),
                                        ({"M": -1}, SHAPE), ({"M": (1 << 20) + 1}, SHAPE), ({"N": 24}, SHAPE), ({"N": 0}, SHAPE), ({"K": 128}, SHAPE), ({"K": 1 << 17}, SHAPE),
-                                       ({"N": 16448, "K": 130816}, SHAPE), ({"dtype": 2}, CONFIG), ({"q": FAKE + 8}, ALIGN), ({"w": FAKE + 8}, ALIGN), ({"ws": FAKE + 2}, ALIGN),
+                                       ({"N": 16448, "K": 130816}, SHAPE), ({"M": 1 << 20, "N": 1 << 22, "K": 256}, SHAPE), ({"dtype": 2}, CONFIG), ({"q": FAKE + 8}, ALIGN), ({"w": FAKE + 8}, ALIGN), ({"ws": FAKE + 2}, ALIGN),
                                        ({"C": FAKE + 8}, ALIGN), ({"work": FAKE + 8}, ALIGN), ({"s": FAKE + 2}, ALIGN), ({}, 0)])
 def test_linear_refusals(kw, status):
     assert _linear(**kw) == status
@@ -344,6 +344,20 @@ def test_product(rtn, M, N, K):
         for n in (0, 4 * M * N * 2, 4 * M * N * 3 + 16):     # sums of whole numbers: the same bits however they are split
             ws = torch.full((max(n, 16) // 16 * 16,), 255, dtype=torch.uint8, device=DEV)
             assert torch.equal(rtn.rtn_linear_w8a8(*args, dtype=dtype, workspace=ws), out)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(1, 512, 28672), (16, 1024, 8192), (64, 1024, 8192), (64, 8192, 28672), (217, 1024, 8192), (1024, 1024, 2048), (33, 4112, 16384)])
+def test_workspaces_are_not_left(rtn, M, N, K):
+    """The splits fit what is given, to the byte, and nothing behind it is touched: all that is asked for, and 16 bytes less than each number of parts takes."""
+    *given, args = _problem(M, N, K, 7)
+    out = rtn.rtn_linear_w8a8(*args)
+    assert _near(out, _product(*given), torch.float16)
+    need = rtn.rtn_linear_w8a8_workspace_nbytes(M, N, K)
+    for n in [need] + [4 * M * N * k - 16 for k in (1, 2, 3, 4, 8)]:
+        buffer = torch.full((n + 4096,), 77, dtype=torch.uint8, device=DEV)
+        assert torch.equal(rtn.rtn_linear_w8a8(*args, workspace=buffer[:n]), out)
+        assert (buffer[n:] == 77).all()
 
 
 @pytest.mark.gpu
