@@ -409,6 +409,59 @@ def report_grouped(args, rtn, synth, torch, np, dev) -> int:
     return 0
 
 
+def report_w8a8(args, rtn, synth, torch, np, dev) -> int:
+    """The 8-bit layer: each projection with 16-bit activations (rtn_linear on the same packed 8-bit weights) and with 8-bit ones (rtn_linear_w8a8), and
+    the calls of rows between them."""
+    shapes = {"8b": synth.LLAMA_8B, "70b": synth.LLAMA_70B, "405b": synth.LLAMA_405B}[args.report_w8a8]
+    print(f"# {args.report_w8a8}, int8 per channel; us per call (HIP-graph replay, weights rotate over 600 MB of copies); w8a16 = rtn_linear, w8a8 = rtn_linear_w8a8")
+
+    def timed(calls):
+        for c in calls:
+            c()
+        torch.cuda.synchronize()
+        cg, st, reps = torch.cuda.CUDAGraph(), torch.cuda.Stream(), max(1, 24 // len(calls))
+        with torch.cuda.stream(st):
+            with torch.cuda.graph(cg, stream=st):
+                for _ in range(reps):
+                    for c in calls:
+                        c()
+        ts = []
+        for _ in range(6):
+            e0, e1 = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            e0.record()
+            cg.replay()
+            e1.record()
+            torch.cuda.synchronize()
+            ts.append(e0.elapsed_time(e1) * 1e3 / (reps * len(calls)))
+        return float(np.median(ts[1:]))
+
+    for name, (K, N) in shapes.items():
+        qw, sc = rtn.rtn_quantize(synth.normal_weight(N, K, 0.02, 1, dev), 8, 0)
+        pool = [qw] + [qw.clone() for _ in range(min(24, int(600e6 // (N * K))))]
+        for M in [int(x) for x in args.batches.split(",")]:
+            x = synth.activation(M, K, 1, dev)
+            q = rtn.rtn_quantize_rows(x)
+            out = torch.empty((M, N), dtype=torch.float16, device=dev)
+            ws = torch.empty(max(rtn.rtn_workspace_nbytes(M, N, K, 8, 0), rtn.rtn_linear_w8a8_workspace_nbytes(M, N, K), 256), dtype=torch.uint8, device=dev)
+            wide = timed([lambda w=w: rtn.rtn_linear(x, w, sc, 8, 0, out=out, workspace=ws) for w in pool])
+            narrow = timed([lambda w=w: rtn.rtn_linear_w8a8(*q, w, sc, out=out, workspace=ws) for w in pool])
+            rows = timed([lambda: rtn.rtn_quantize_rows(x, out=q)])
+            rate, tops = (N * K + M * K + 2 * M * N) / narrow / 1e3, 2e-6 * M * N * K / narrow
+            print(f"{name:8s} {K:6d}->{N:6d} M={M:5d}  w8a16 {wide:9.2f}  w8a8 {narrow:9.2f}  {wide / narrow:5.2f}x  {rate:6.0f} GB/s {tops:6.0f} TFLOP/s | rows quantised {rows:7.2f}", flush=True)
+        del pool, qw
+    H, F = shapes["qkv"][0], shapes["down"][0]
+    weight = torch.ones(H, dtype=torch.float16, device=dev)
+    for M in [int(x) for x in args.batches.split(",")]:
+        x, r, up = synth.activation(M, H, 1, dev), synth.activation(M, H, 2, dev), synth.activation(M, 2 * F, 3, dev)
+        to = torch.empty((M, H), dtype=torch.int8, device=dev), torch.empty(M, device=dev)
+        gated = torch.empty((M, F), dtype=torch.int8, device=dev), torch.empty(M, device=dev)
+        summed = torch.empty_like(r)
+        norm = timed([lambda: rtn.rtn_norm_rows(x, weight, residual=r, residual_out=summed, quantize=True, out=to)])
+        act = timed([lambda: rtn.rtn_gated_rows(up, quantize=True, out=gated)])
+        print(f"rows M={M:5d}  norm of {H} with residual {norm:7.2f} ({7 * M * H / norm / 1e3:6.0f} GB/s)  gated activation of {F} {act:7.2f} ({5 * M * F / act / 1e3:6.0f} GB/s)", flush=True)
+    return 0
+
+
 def report_attention(args, rtn, synth, torch, np, dev) -> int:
     """A layer's attention block in token generation: rtn_cache_plan once a step, then the quantised QKV projection, rotation with the cache
     write, attention over the pages and the quantised output projection, captured and replayed while the requests grow."""
@@ -500,6 +553,8 @@ def main() -> int:
                     help="instead of the JSON line, time expert-like independent modules serially and through the grouped call")
     ap.add_argument("--report-attention", choices=["8b", "70b", "405b"], default=None,
                     help="a layer's attention block in token generation over a paged KV cache: projections, rotation, attention")
+    ap.add_argument("--report-w8a8", choices=["8b", "70b", "405b"], default=None,
+                    help="per-projection table of the 8-bit layer (activations in 16 and in 8 bits on the same weights) and its calls of rows")
     ap.add_argument("--bits", type=int, default=4, help="--report only: 4 (group 128) or 8 (per-channel)")
     ap.add_argument("--selective", action="store_true",
                     help="--report only: the selective-precision layer (modules 2 and 4 at 8 bit per-channel, the others at 4 bit g128)")
@@ -531,6 +586,8 @@ def main() -> int:
         return report_load(args, rtn, synth, torch, np, dev)
     if args.report_attention:
         return report_attention(args, rtn, synth, torch, np, dev)
+    if args.report_w8a8:
+        return report_w8a8(args, rtn, synth, torch, np, dev)
     if args.report_grouped:
         return report_grouped(args, rtn, synth, torch, np, dev)
     if args.report_ceiling:

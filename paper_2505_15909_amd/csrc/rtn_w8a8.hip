@@ -34,7 +34,8 @@ __device__ __forceinline__ u32x2_t four_results(int4_t sum, float row_scale, hal
 
 // Workgroups on other columns read the same activations, and with K a power of two their weights start on the same memory channels.  Each begins at another place of
 // its n steps along K and goes round (sums of whole numbers have no order).  16 rows of 28672 x 4096 26.0 -> 20.9 us, 64 rows 26.2 -> 22.0; 16 rows of 28672 x
-// 8192 41.3 -> 37.7; where K is no power of two the same to 3 % (K = 4352: 21.5 and 22.6).  Tiles, whose neighbours take turns on an L2's contents, are 2 % slower that way.
+// 8192 41.3 -> 37.7; where K is no power of two the same to 3 % (K = 4352: 21.5 and 22.6).  Tiles only where a round holds them all: in more,
+// neighbours take turns on an L2's contents (8192 rows 2 % slower).
 __device__ __forceinline__ int first_step(int column_tile, int n) { return (int)__umulhi((uint32_t)column_tile * 2654435769u, (uint32_t)n); }
 __device__ __forceinline__ int around(int i, int n) { return i < n ? i : i - n; }
 
@@ -190,6 +191,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
     const int m0 = yb * TM, n0 = xb * kTileN, K = p.KT * 64;
     const int pairs = p.KT / 4;                              // (two steps each: a workgroup has an even number of them)
     const int s0 = 2 * (int)((int64_t)pairs * z / p.split), T = 2 * (int)((int64_t)pairs * (z + 1) / p.split) - s0;
+    const int begin = p.XB * p.YB * p.split <= 256 ? first_step(xb, T) : 0;
 
     // Both operands through resources that start at this workgroup's first row; rows past M or N read zeros, steps past the last one the last.
     const int a_rows = min(TM, p.M - m0), b_tiles = min(kTileN, p.N - n0) / 16;
@@ -208,9 +210,9 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
         const int row = wave * (NB / 2) + i;
         b_lane[i] = row < b_tiles ? (uint32_t)row * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
     }
-    auto a_dma = [&](int stage, int t, int i) { load_to_lds(ra, stage_a(stage) + (wave * NA + i) * 1024, a_lane[i], (s0 + min(t, T - 1)) * 128); };
+    auto a_dma = [&](int stage, int t, int i) { load_to_lds(ra, stage_a(stage) + (wave * NA + i) * 1024, a_lane[i], (s0 + around(begin + min(t, T - 1), T)) * 128); };
     auto b_dma = [&](int stage, int t, int i) {
-        load_to_lds(rb, stage_b(stage) + (wave * NB + i) * 1024, b_lane[i >> 1], (s0 + min(t, T - 1)) * 2048 + (i & 1) * 1024);
+        load_to_lds(rb, stage_b(stage) + (wave * NB + i) * 1024, b_lane[i >> 1], (s0 + around(begin + min(t, T - 1), T)) * 2048 + (i & 1) * 1024);
     };
 
     int4_t acc[MBW][4];
@@ -501,22 +503,23 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 // (each + more x the share of a workgroup's rows that M has), a unit being the 64 (128) columns of a step of each wavefront along K: a compute unit
 // has some 32 KiB on their way at once, 50 to 65 GB/s where they come from beyond its L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup
 // a compute unit, whose step takes `each` where half the chip is busy and `each + more` where all of it is (power).  That against the weights' stream,
-// and a K split's join.  Fitted to 20 000 launches over 750 problems (1 to 8192 rows, 256 to 57344 columns, K 1024 to 28672): 7 to 11 % rms (15 for
-// 64 rows with four wavefronts along K), and the pick is 1.8 % behind the best of all launches on the mean, 24 % at most.
+// and a K split's join.  Fitted to 35 000 launches over 1400 problems (1 to 8192 rows, 256 to 57344 columns, K 1024 to 28672): 7 to 12 % rms (15 for
+// 64 rows with four wavefronts along K), and the pick is 2.2 % behind the best of all launches on the mean, 29 % at most.
 enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
 struct W8A8Shape {
     int kind, mb, nt, wk, depth;
     float start, each, more;
 };
 constexpr W8A8Shape kShapes[] = {
-    {W8A8_STREAM, 1, 1, 8, 4, 3.38f, 0.129f, 0.219f}, {W8A8_STREAM, 1, 1, 8, 2, 3.33f, 0.179f, 0.159f}, {W8A8_STREAM, 1, 2, 8, 2, 3.16f, 0.294f, 0.236f},
-    {W8A8_STREAM, 1, 4, 8, 2, 3.09f, 0.625f, 0.244f}, {W8A8_STREAM, 2, 2, 8, 2, 3.00f, 0.399f, 0.392f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.36f, 0.479f, 0.059f},
-    {W8A8_BLOCK, 2, 2, 4, 3, 3.28f, 0.881f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 3.95f, 0.696f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.35f, 0.496f, 0.406f},
-    {W8A8_BLOCK, 4, 1, 2, 3, 3.98f, 0.436f, 0.129f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.42f, 0.364f, 0.104f},  {W8A8_BLOCK, 4, 2, 2, 3, 4.75f, 0.793f, 0.115f},
-    {W8A8_BLOCK, 4, 2, 1, 3, 5.11f, 0.715f, 0.051f},  {W8A8_BLOCK, 8, 2, 2, 3, 7.21f, 1.006f, 0.260f},  {W8A8_TILE, 4, 0, 0, 0, 5.60f, 0.719f, 0.186f},
-    {W8A8_TILE, 8, 0, 0, 0, 7.85f, 1.066f, 0.431f}};
+    {W8A8_STREAM, 1, 1, 8, 4, 3.44f, 0.129f, 0.219f}, {W8A8_STREAM, 1, 1, 8, 2, 3.42f, 0.177f, 0.158f}, {W8A8_STREAM, 1, 2, 8, 2, 3.23f, 0.295f, 0.228f},
+    {W8A8_STREAM, 1, 4, 8, 2, 3.16f, 0.621f, 0.239f}, {W8A8_STREAM, 2, 2, 8, 2, 3.11f, 0.383f, 0.399f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.52f, 0.497f, 0.015f},
+    {W8A8_BLOCK, 2, 2, 4, 3, 3.42f, 0.852f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.00f, 0.681f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.52f, 0.535f, 0.319f},
+    {W8A8_BLOCK, 4, 1, 2, 3, 4.01f, 0.424f, 0.130f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.46f, 0.356f, 0.102f},  {W8A8_BLOCK, 4, 2, 2, 3, 4.77f, 0.807f, 0.081f},
+    {W8A8_BLOCK, 4, 2, 1, 3, 5.14f, 0.742f, 0.012f},  {W8A8_BLOCK, 8, 1, 1, 3, 6.60f, 0.571f, 0.060f},  {W8A8_BLOCK, 8, 2, 2, 3, 7.41f, 1.038f, 0.194f},
+    {W8A8_BLOCK, 8, 2, 1, 3, 7.46f, 0.945f, 0.031f},  {W8A8_TILE, 4, 0, 0, 0, 5.44f, 0.721f, 0.173f},   {W8A8_TILE, 8, 0, 0, 0, 7.49f, 1.048f, 0.439f}};
 // Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
-constexpr float kSharedStream = 1.209f, kSharedNear = 0.706f, kSharedFar = 0.957f;
+// A tile kernel's one row tile, which has the weights to itself, the last.
+constexpr float kSharedStream = 1.208f, kSharedNear = 0.723f, kSharedFar = 0.980f, kTileAlone = 1.071f;
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 struct W8A8Plan {
@@ -543,7 +546,7 @@ static bool weights_near(int64_t N, int64_t K) { return N * K <= (int64_t)32 << 
 static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
     W8A8Plan plan = {};
     float best = 1e30f;
-    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.12e6f);
+    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.16e6f);
     const float s4 = stream * stream * stream * stream;
     const int splits = (int)std::min<uint64_t>(8, std::min(workspace, kW8A8Workspace) / 4 / (uint64_t)(M * N));
     const int pieces = (int)((M + 15) / 16);
@@ -556,7 +559,7 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
         const int64_t XB = up(N, c.columns), YB = up(M, c.rows), tiles = XB * YB, all_units = K >> c.unit;
         const float shared = YB == 1 ? 1.f : k.kind == W8A8_STREAM ? kSharedStream : weights_near(N, K) ? kSharedNear : kSharedFar;
         const float unit_us = (k.each + k.more * (float)M / (float)(YB << c.rows)) * shared;
-        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 2.81e6f));
+        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 3.28e6f));
         for (int split = 1; split <= std::max(1, splits); ++split) {
             if (split > 1 && ((split << c.along) > all_units || tiles * split > 800)) break;
             const float steps = (float)up((uint32_t)(all_units + split - 1) / (uint32_t)split, c.along);
@@ -564,12 +567,13 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
             if (k.kind == W8A8_TILE) {
                 const int64_t on_xcd = up(tiles, 3) * split;
                 const float part = (float)(on_xcd & 31) * (1.f / 32.f);
-                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 5.54f) - 5.54f;
-                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 5.54f;
+                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 5.12f) - 5.12f;
+                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 5.12f;
+                if (YB == 1) work *= kTileAlone;
             } else {
                 work = steps * unit_us * (float)(k.kind == W8A8_STREAM ? up(tiles * split, 8) : up(up(tiles, 3) * split, 5));
             }
-            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 3.90f : 2.77f) + (outputs + 4.f * outputs * (float)split) * (1.f / 6.76e6f) : 0.f);
+            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 4.11f : 2.80f) + (outputs + 4.f * outputs * (float)split) * (1.f / 7.09e6f) : 0.f);
             if (rest + std::max(work, stream) >= best) continue;
             const float t = rest + std::sqrt(std::sqrt(work * work * work * work + s4));
             if (t < best) {
