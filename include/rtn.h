@@ -427,7 +427,7 @@ rtn_status rtn_quantize_rows(const void* dev_x, int64_t rows, int64_t x_stride, 
 /* out[m, k] = code[m, k] * scale[m], rounded once to the type: for a module that takes 16 bits beside one that takes 8. */
 rtn_status rtn_dequantize_rows(const void* dev_q, const float* dev_q_scales, int64_t rows, int64_t dim, int dtype, void* dev_out, void* stream);
 
-/* C[m, n] = T( (sum_k q[m, k] * w[n, k]) * (q_scale[m] * scale[n]) ), the sum exact in 32-bit integers, the rest in fp32, rounded once.
+/* C[m, n] = T( (sum_k q[m, k] * w[n, k]) * q_scale[m] * scale[n] ), the sum exact in 32-bit integers, the products in this order in fp32, rounded once to T.
  *   dev_q          in   int8 [M, K] row-major (any codes, -128 included); dev_q_scales fp32 [M]
  *   dev_qweight    in   packed 8-bit codes [N, K] of rtn_quantize with one group a row; dev_scales fp16 [N]
  *   dev_C          out  [M, N] in `dtype`, RTN_TYPE_F16 or RTN_TYPE_BF16

@@ -1,4 +1,4 @@
-// Products of 8-bit rows with packed 8-bit weights: C = T(sum_k q_a q_w * (S_a S_w)), sums in 32-bit integers.
+// Products of 8-bit rows with packed 8-bit weights: C = T(sum_k q_a q_w * S_a * S_w), sums in 32-bit integers.
 //
 // v_mfma_i32_16x16x64_i8 takes 16 bytes a lane of each side: row (lane & 15), and the same 16 columns of 64 on both sides, in any order.  A packed
 // tile is 16 rows x 64 columns and lane (row, quarter kq) owns the columns 8 kq .. and 32 + 8 kq .., codes + 128.  Two v_permlane16_swap
@@ -28,7 +28,7 @@ __device__ __forceinline__ u32x2_t four_results(int4_t sum, float row_scale, hal
     typedef typename Elem<TYPE>::one E;
     E4 y;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = (E)((float)sum[e] * (row_scale * (float)s[e]));
+    for (int e = 0; e < 4; ++e) y[e] = (E)((float)sum[e] * row_scale * (float)s[e]);
     return __builtin_bit_cast(u32x2_t, y);
 }
 

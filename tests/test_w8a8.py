@@ -9,7 +9,7 @@ up to 2^-25.
   mean, rsqrt (one unit = 2 e), and two roundings behind it: 43 + 1 + 2 + 2, bounded by 50 e.
   The gate: gelu's z comes from two constants and five operations, each e, so that it is off by at most 7 e |z| (silu's z is exact), which exp carries over; exp's own error
   2 e, 1 + exp, the quotient and the product with b 1 e each, and 3 e to spare: (8 + 7 |z|) e relative.  Below 2^-120 |b| results may vanish.
-  The product: the sum is exact; it, the scales' product and the result's are rounded in fp32: 3 e, and then u."""
+  The product: the sum is exact; it and its two products with scales are rounded in fp32: 3 e, and then u."""
 import numpy as np
 import pytest
 import torch
