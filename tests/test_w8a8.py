@@ -392,6 +392,37 @@ def test_product_of_what_the_quantisers_give(rtn, M, N, K, flags):
     assert ((want - true).abs() <= slack).all()
 
 
+@pytest.mark.gpu
+def test_offsets_beyond_32_bits(rtn):
+    """Rows, codes and results whose offsets pass 32 bits: the last rows are what a call of their own gives."""
+    M, K = 70001, 40960
+    x = torch.empty(M, K, dtype=torch.bfloat16, device=DEV)
+    x[:-3] = 1.0
+    x[-3:] = torch.randn(3, K, device=DEV)
+    w = torch.randn(K, device=DEV).bfloat16()
+    q, s = rtn.rtn_quantize_rows(x)
+    few = rtn.rtn_quantize_rows(x[-3:])
+    assert torch.equal(q[-3:], few[0]) and torch.equal(s[-3:], few[1]) and (q[M // 2] == 127).all()
+    assert torch.equal(rtn.rtn_dequantize_rows(q, s, torch.bfloat16)[-3:], rtn.rtn_dequantize_rows(*few, torch.bfloat16))
+    few = rtn.rtn_gated_rows(x[-3:], quantize=True)
+    got = rtn.rtn_gated_rows(x, quantize=True)
+    assert torch.equal(got[0][-3:], few[0]) and torch.equal(got[1][-3:], few[1])
+    r = x[-3:].clone()
+    y = rtn.rtn_norm_rows(r.clone(), w, residual=r)
+    assert torch.equal(rtn.rtn_norm_rows(x, w, residual=x)[-3:], y) and torch.equal(x[-3:], r)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("M,N,K", [(80001, 28672, 256), (1 << 20, 16, 4096), (1 << 20, 272, 2304)])
+def test_products_whose_offsets_pass_32_bits(rtn, M, N, K):
+    *_, (qe, se, qw, ws) = _problem(5, N, K, 3)
+    q, s = torch.ones(M, K, dtype=torch.int8, device=DEV), torch.ones(M, device=DEV)
+    q[-5:], s[-5:] = qe, se
+    out = rtn.rtn_linear_w8a8(q, s, qw, ws)
+    assert torch.equal(out[-5:], rtn.rtn_linear_w8a8(qe, se, qw, ws))
+    assert torch.equal(out[M // 2], out[0]) and torch.equal(out[:1], rtn.rtn_linear_w8a8(q[:1], s[:1], qw, ws))
+
+
 # ---- together, on streams, in graphs ------------------------------------------------------------------------------------------------
 
 def _layer(rtn, seed, H=512, F=1280, heads=4, kv=2, D=128):
