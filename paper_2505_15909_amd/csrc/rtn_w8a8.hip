@@ -60,7 +60,9 @@ constexpr int kStreaming = 2;                                // read once
 
 // ---- Few rows: bound by the stream of weights.  A wavefront multiplies NT tile rows of weights by MB blocks of 16 rows, both straight
 // from memory into registers, D tiles ahead; the WK wavefronts of a workgroup take the tiles of its K range in turn (what they read
-// together is in one piece), and add up in LDS. ----
+// together is in one piece), and add up in LDS.  No wavefront waits for another before the end.  More tile rows to a wavefront (NT) fetch the activations less often,
+// fewer make more workgroups: 8 rows of 106496 x 16384 (NT 1, 2, 4) 302, 253, 263 us, 16 rows of 28672 x 4096 27, 22, 21, one row of 4096 x 4096 5.0, 7.2, 8.
+// 6.8 to 7 TB/s on the large ones; 20 us for one row of 28672 x 4096 (5.8 TB/s). ----
 template <int TYPE, int MB, int NT, int WK, int D>
 __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p) {
     __shared__ __align__(16) int4_t sums[WK * MB * NT * 64];
@@ -155,7 +157,10 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
 // LDS (piece_at); packed tiles lie as they are, a lane reads its own chunk.  Both come
 // straight into LDS, SA and SB steps ahead.  A step runs in phases of two row blocks and both halves of its columns; a phase reads the next one's operands, and
 // the one barrier of a step stands before its last phase, whose operands are in registers by then: the stage is free behind it, and the
-// requests for it go out over the phases that follow. ----
+// requests for it go out over the phases that follow.  8192 rows of 28672 x 4096 700 to 750 us on different cards (2.6 to 2.75 PFLOP/s), 8192 x 8192 x 8192 373
+// to 399 (2.95), where the vendor library's int8 product takes 988 and 445; matrix cores 69 % busy at 1.65 GHz.  Turning weights into operands
+// costs 6 % of that.  A round of tiles begins and ends for 5 us (K = 4096: 10 %): workgroups that stay and request the next tile's first steps under the last
+// one's end have registers for two stages of weights only, and lose more on every step than they gain (749 -> 791; K = 512 170 -> 161). ----
 constexpr int kTileN = 256, kTileThreads = 512;
 constexpr int kZGroup = 4;
 
@@ -364,7 +369,8 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
 // ---- Rows between: bound by the stream of weights where enough of them is on its way.  The eight wavefronts of a workgroup stand 8 / WK along N and WK along K.
 // A wavefront has NT tile rows of weights, straight into registers; the activations, 16 MB rows, come into LDS once for the wavefronts along N.
 // A step is 128 columns for each wavefront along K; both are requested S - 1 steps ahead, and one barrier a step says that its activations have landed
-// and the last one's are used up.  The wavefronts along K add up in LDS at the end.  ONCE: the weights are marked as read once -- one row tile, or more weights
+// and the last one's are used up.  The wavefronts along K add up in LDS at the end, so that a small matrix fills the chip without a join: 217 rows of 4096 x 4096 10.6 us
+// (two along K, 256 workgroups; one 16.1, tiles 20.7), 128 rows 8.3 (four).  64 rows of 28672 x 4096 22 us (5.5 TB/s), 128 rows 28.  ONCE: the weights are marked as read once -- one row tile, or more weights
 // than the L2s hold: 64 rows of 8192 x 28672 43.9 us, 46.8 unmarked; marked where two row tiles share them, 128 rows of 4096 x 4096 take 9.6 for 8.3,
 // 160 of 5120 x 5120 14.0 for 12.0. ----
 template <int TYPE, int MB, int NT, int WK, int S, bool ONCE>
