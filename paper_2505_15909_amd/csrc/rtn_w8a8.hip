@@ -492,15 +492,23 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
     }
 }
 
+constexpr int kMostSplits = 8;
+
 // Sums of the K splits' parts, four columns a thread.
 template <int TYPE>
 __global__ __launch_bounds__(256) void w8a8_join_kernel(const W8A8Params p) {
     const int64_t all = (int64_t)p.M * p.N, at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
     if (at >= all) return;
-    int4_t s = *reinterpret_cast<const int4_t*>(p.ws + at);
-    for (int z = 1; z < p.split; ++z) s += *reinterpret_cast<const int4_t*>(p.ws + z * all + at);
+    int4_t part[kMostSplits];                                // all requested before the first is added
+#pragma unroll
+    for (int z = 0; z < kMostSplits; ++z) part[z] = z < p.split ? *reinterpret_cast<const int4_t*>(p.ws + z * all + at) : (int4_t){0, 0, 0, 0};
     const int m = (int)(at / p.N), c = (int)(at - (int64_t)m * p.N);
-    *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, p.a_scales[m], *reinterpret_cast<const half4_t*>(p.scales + c));
+    const float row_scale = p.a_scales[m];
+    const half4_t scale = *reinterpret_cast<const half4_t*>(p.scales + c);
+    int4_t s = part[0];
+#pragma unroll
+    for (int z = 1; z < kMostSplits; ++z) s += part[z];
+    *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, row_scale, scale);
 }
 
 constexpr size_t kW8A8Workspace = (size_t)64 << 20;
@@ -509,23 +517,23 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 // (each + more x the share of a workgroup's rows that M has), a unit being the 64 (128) columns of a step of each wavefront along K: a compute unit
 // has some 32 KiB on their way at once, 50 to 65 GB/s where they come from beyond its L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup
 // a compute unit, whose step takes `each` where half the chip is busy and `each + more` where all of it is (power).  That against the weights' stream,
-// and a K split's join.  Fitted to 35 000 launches over 1400 problems (1 to 8192 rows, 256 to 57344 columns, K 1024 to 28672): 7 to 12 % rms (15 for
-// 64 rows with four wavefronts along K), and the pick is 2.2 % behind the best of all launches on the mean, 29 % at most.
+// and a K split's join.  Fitted to 47 000 launches over 1600 problems (1 to 8192 rows, 128 to 57344 columns, K 768 to 28672): 8 to 13 % rms (15 for
+// 64 rows with four wavefronts along K), and the pick is 1.8 % behind the best of all launches on the mean (2.8 % below 2000 columns), 27 % at most.
 enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
 struct W8A8Shape {
     int kind, mb, nt, wk, depth;
     float start, each, more;
 };
 constexpr W8A8Shape kShapes[] = {
-    {W8A8_STREAM, 1, 1, 8, 4, 3.44f, 0.129f, 0.219f}, {W8A8_STREAM, 1, 1, 8, 2, 3.42f, 0.177f, 0.158f}, {W8A8_STREAM, 1, 2, 8, 2, 3.23f, 0.295f, 0.228f},
-    {W8A8_STREAM, 1, 4, 8, 2, 3.16f, 0.621f, 0.239f}, {W8A8_STREAM, 2, 2, 8, 2, 3.11f, 0.383f, 0.399f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.52f, 0.497f, 0.015f},
-    {W8A8_BLOCK, 2, 2, 4, 3, 3.42f, 0.852f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.00f, 0.681f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.52f, 0.535f, 0.319f},
-    {W8A8_BLOCK, 4, 1, 2, 3, 4.01f, 0.424f, 0.130f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.46f, 0.356f, 0.102f},  {W8A8_BLOCK, 4, 2, 2, 3, 4.77f, 0.807f, 0.081f},
-    {W8A8_BLOCK, 4, 2, 1, 3, 5.14f, 0.742f, 0.012f},  {W8A8_BLOCK, 8, 1, 1, 3, 6.60f, 0.571f, 0.060f},  {W8A8_BLOCK, 8, 2, 2, 3, 7.41f, 1.038f, 0.194f},
-    {W8A8_BLOCK, 8, 2, 1, 3, 7.46f, 0.945f, 0.031f},  {W8A8_TILE, 4, 0, 0, 0, 5.44f, 0.721f, 0.173f},   {W8A8_TILE, 8, 0, 0, 0, 7.49f, 1.048f, 0.439f}};
+    {W8A8_STREAM, 1, 1, 8, 4, 3.47f, 0.126f, 0.218f}, {W8A8_STREAM, 1, 1, 8, 2, 3.46f, 0.174f, 0.153f}, {W8A8_STREAM, 1, 2, 8, 2, 3.27f, 0.285f, 0.228f},
+    {W8A8_STREAM, 1, 4, 8, 2, 3.19f, 0.607f, 0.239f}, {W8A8_STREAM, 2, 2, 8, 2, 3.21f, 0.410f, 0.346f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.53f, 0.492f, 0.f},
+    {W8A8_BLOCK, 2, 2, 4, 3, 3.50f, 0.810f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.13f, 0.653f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.45f, 0.545f, 0.301f},
+    {W8A8_BLOCK, 4, 1, 2, 3, 4.10f, 0.392f, 0.166f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.62f, 0.334f, 0.123f},  {W8A8_BLOCK, 4, 2, 2, 3, 4.92f, 0.775f, 0.100f},
+    {W8A8_BLOCK, 4, 2, 1, 3, 5.36f, 0.727f, 0.008f},  {W8A8_BLOCK, 8, 1, 1, 3, 7.00f, 0.535f, 0.099f},  {W8A8_BLOCK, 8, 2, 2, 3, 7.75f, 0.986f, 0.240f},
+    {W8A8_BLOCK, 8, 2, 1, 3, 7.93f, 0.894f, 0.074f},  {W8A8_TILE, 4, 0, 0, 0, 5.51f, 0.716f, 0.173f},   {W8A8_TILE, 8, 0, 0, 0, 7.31f, 1.062f, 0.414f}};
 // Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
 // A tile kernel's one row tile, which has the weights to itself, the last.
-constexpr float kSharedStream = 1.208f, kSharedNear = 0.723f, kSharedFar = 0.980f, kTileAlone = 1.071f;
+constexpr float kSharedStream = 1.203f, kSharedNear = 0.725f, kSharedFar = 0.987f, kTileAlone = 1.071f;
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 struct W8A8Plan {
@@ -552,20 +560,21 @@ static bool weights_near(int64_t N, int64_t K) { return N * K <= (int64_t)32 << 
 static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
     W8A8Plan plan = {};
     float best = 1e30f;
-    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.16e6f);
+    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.13e6f);
     const float s4 = stream * stream * stream * stream;
-    const int splits = (int)std::min<uint64_t>(8, std::min(workspace, kW8A8Workspace) / 4 / (uint64_t)(M * N));
+    const int splits = (int)std::min<uint64_t>(kMostSplits, std::min(workspace, kW8A8Workspace) / 4 / (uint64_t)(M * N));
     const int pieces = (int)((M + 15) / 16);
+    const bool near = weights_near(N, K);
     auto up = [](int64_t n, int log2) { return (n + ((int64_t)1 << log2) - 1) >> log2; };
     for (int i = 0; i < kShapeCount; ++i) {
         const W8A8Shape& k = kShapes[i];
         const W8A8Cover& c = kCovers[i];
         if ((1 << c.rows) >= 32 * pieces && c.rows > 5) continue;            // mostly rows beyond M
-        if (k.kind != W8A8_TILE && pieces > 8 << (c.rows - 4)) continue;     // the weights eight times and more
+        if (k.kind != W8A8_TILE && pieces > (near ? 128 : 8) << (c.rows - 4)) continue;      // (that many times the weights)
         const int64_t XB = up(N, c.columns), YB = up(M, c.rows), tiles = XB * YB, all_units = K >> c.unit;
-        const float shared = YB == 1 ? 1.f : k.kind == W8A8_STREAM ? kSharedStream : weights_near(N, K) ? kSharedNear : kSharedFar;
+        const float shared = YB == 1 ? 1.f : k.kind == W8A8_STREAM ? kSharedStream : near ? kSharedNear : kSharedFar;
         const float unit_us = (k.each + k.more * (float)M / (float)(YB << c.rows)) * shared;
-        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 3.28e6f));
+        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 3.67e6f));
         for (int split = 1; split <= std::max(1, splits); ++split) {
             if (split > 1 && ((split << c.along) > all_units || tiles * split > 800)) break;
             const float steps = (float)up((uint32_t)(all_units + split - 1) / (uint32_t)split, c.along);
@@ -573,13 +582,13 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
             if (k.kind == W8A8_TILE) {
                 const int64_t on_xcd = up(tiles, 3) * split;
                 const float part = (float)(on_xcd & 31) * (1.f / 32.f);
-                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 5.12f) - 5.12f;
-                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 5.12f;
+                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 4.88f) - 4.88f;
+                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 4.88f;
                 if (YB == 1) work *= kTileAlone;
             } else {
                 work = steps * unit_us * (float)(k.kind == W8A8_STREAM ? up(tiles * split, 8) : up(up(tiles, 3) * split, 5));
             }
-            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 4.11f : 2.80f) + (outputs + 4.f * outputs * (float)split) * (1.f / 7.09e6f) : 0.f);
+            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 3.91f : 2.96f) + (outputs + 4.f * outputs * (float)split) * (1.f / 6.87e6f) : 0.f);
             if (rest + std::max(work, stream) >= best) continue;
             const float t = rest + std::sqrt(std::sqrt(work * work * work * work + s4));
             if (t < best) {
