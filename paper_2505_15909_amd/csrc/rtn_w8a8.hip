@@ -517,28 +517,30 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 // (each + more x the share of a workgroup's rows that M has), a unit being the 64 (128) columns of a step of each wavefront along K: a compute unit
 // has some 32 KiB on their way at once, 50 to 65 GB/s where they come from beyond its L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup
 // a compute unit, whose step takes `each` where half the chip is busy and `each + more` where all of it is (power).  That against the weights' stream,
-// and a K split's join.  Fitted to 47 000 launches over 1600 problems (1 to 8192 rows, 128 to 57344 columns, K 768 to 28672): 8 to 13 % rms (15 for
-// 64 rows with four wavefronts along K), and the pick is 1.8 % behind the best of all launches on the mean (2.8 % below 2000 columns), 27 % at most.
+// and a K split's join.  Fitted to 57 000 launches over 2000 problems (1 to 8192 rows, 128 to 57344 columns, K 768 to 28672): 7 to 13 % rms (19 for
+// 16 wavefronts along K), and the pick is 2 % behind the best of all launches on the mean (1 % from 129 rows, 3.5 % up to 40 rows and below 2000 columns), 32 % at most.
 enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
 struct W8A8Shape {
     int kind, mb, nt, wk, depth;
     float start, each, more;
 };
 constexpr W8A8Shape kShapes[] = {
-    {W8A8_STREAM, 1, 1, 8, 4, 3.47f, 0.126f, 0.218f}, {W8A8_STREAM, 1, 1, 8, 2, 3.46f, 0.174f, 0.153f}, {W8A8_STREAM, 1, 2, 8, 2, 3.27f, 0.285f, 0.228f},
-    {W8A8_STREAM, 1, 4, 8, 2, 3.19f, 0.607f, 0.239f}, {W8A8_STREAM, 2, 2, 8, 2, 3.21f, 0.410f, 0.346f}, {W8A8_BLOCK, 2, 1, 4, 3, 3.53f, 0.492f, 0.f},
-    {W8A8_BLOCK, 2, 2, 4, 3, 3.50f, 0.810f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.13f, 0.653f, 0.f},     {W8A8_BLOCK, 4, 1, 4, 3, 3.45f, 0.545f, 0.301f},
-    {W8A8_BLOCK, 4, 1, 2, 3, 4.10f, 0.392f, 0.166f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.62f, 0.334f, 0.123f},  {W8A8_BLOCK, 4, 2, 2, 3, 4.92f, 0.775f, 0.100f},
-    {W8A8_BLOCK, 4, 2, 1, 3, 5.36f, 0.727f, 0.008f},  {W8A8_BLOCK, 8, 1, 1, 3, 7.00f, 0.535f, 0.099f},  {W8A8_BLOCK, 8, 2, 2, 3, 7.75f, 0.986f, 0.240f},
-    {W8A8_BLOCK, 8, 2, 1, 3, 7.93f, 0.894f, 0.074f},  {W8A8_TILE, 4, 0, 0, 0, 5.51f, 0.716f, 0.173f},   {W8A8_TILE, 8, 0, 0, 0, 7.31f, 1.062f, 0.414f}};
+    {W8A8_STREAM, 1, 1, 16, 4, 3.81f, 0.257f, 0.34f}, {W8A8_STREAM, 1, 1, 8, 4, 3.53f, 0.127f, 0.21f},  {W8A8_STREAM, 1, 1, 8, 2, 3.52f, 0.177f, 0.143f},
+    {W8A8_STREAM, 1, 2, 8, 2, 3.32f, 0.285f, 0.218f}, {W8A8_STREAM, 1, 4, 8, 2, 3.22f, 0.609f, 0.222f}, {W8A8_STREAM, 2, 2, 8, 2, 3.21f, 0.432f, 0.311f},
+    {W8A8_BLOCK, 2, 1, 4, 3, 3.52f, 0.494f, 0.f},     {W8A8_BLOCK, 2, 2, 4, 3, 3.45f, 0.815f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.05f, 0.655f, 0.f},
+    {W8A8_BLOCK, 4, 1, 4, 3, 3.38f, 0.543f, 0.31f},   {W8A8_BLOCK, 4, 1, 2, 3, 4.01f, 0.395f, 0.168f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.43f, 0.343f, 0.12f},
+    {W8A8_BLOCK, 4, 2, 2, 3, 4.75f, 0.797f, 0.082f},  {W8A8_BLOCK, 4, 2, 1, 3, 5.02f, 0.743f, 0.f},     {W8A8_BLOCK, 8, 1, 1, 3, 6.59f, 0.555f, 0.088f},
+    {W8A8_BLOCK, 8, 2, 2, 3, 7.39f, 1.017f, 0.227f},  {W8A8_BLOCK, 8, 2, 1, 3, 7.55f, 0.92f, 0.056f},   {W8A8_TILE, 4, 0, 0, 0, 5.53f, 0.715f, 0.169f},
+    {W8A8_TILE, 8, 0, 0, 0, 7.3f, 1.063f, 0.405f}};
 // Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
 // A tile kernel's one row tile, which has the weights to itself, the last.
-constexpr float kSharedStream = 1.203f, kSharedNear = 0.725f, kSharedFar = 0.987f, kTileAlone = 1.071f;
+constexpr float kSharedStream = 1.200f, kSharedNear = 0.715f, kSharedFar = 0.979f, kTileAlone = 1.073f;
 constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
 
 struct W8A8Plan {
     int shape, split;
     int64_t XB, YB;
+    int threads() const { return kShapes[shape].kind == W8A8_STREAM ? kShapes[shape].wk * 64 : 512; }
     int64_t workgroups() const { return (kShapes[shape].kind == W8A8_STREAM ? XB * YB : (XB * YB + kXcds - 1) / kXcds * kXcds) * split; }
 };
 
@@ -560,7 +562,7 @@ static bool weights_near(int64_t N, int64_t K) { return N * K <= (int64_t)32 << 
 static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
     W8A8Plan plan = {};
     float best = 1e30f;
-    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.13e6f);
+    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.14e6f);
     const float s4 = stream * stream * stream * stream;
     const int splits = (int)std::min<uint64_t>(kMostSplits, std::min(workspace, kW8A8Workspace) / 4 / (uint64_t)(M * N));
     const int pieces = (int)((M + 15) / 16);
@@ -574,7 +576,7 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
         const int64_t XB = up(N, c.columns), YB = up(M, c.rows), tiles = XB * YB, all_units = K >> c.unit;
         const float shared = YB == 1 ? 1.f : k.kind == W8A8_STREAM ? kSharedStream : near ? kSharedNear : kSharedFar;
         const float unit_us = (k.each + k.more * (float)M / (float)(YB << c.rows)) * shared;
-        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 3.67e6f));
+        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 3.06e6f));
         for (int split = 1; split <= std::max(1, splits); ++split) {
             if (split > 1 && ((split << c.along) > all_units || tiles * split > 800)) break;
             const float steps = (float)up((uint32_t)(all_units + split - 1) / (uint32_t)split, c.along);
@@ -582,19 +584,23 @@ static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
             if (k.kind == W8A8_TILE) {
                 const int64_t on_xcd = up(tiles, 3) * split;
                 const float part = (float)(on_xcd & 31) * (1.f / 32.f);
-                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 4.88f) - 4.88f;
-                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 4.88f;
+                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 4.91f) - 4.91f;
+                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 4.91f;
                 if (YB == 1) work *= kTileAlone;
             } else {
                 work = steps * unit_us * (float)(k.kind == W8A8_STREAM ? up(tiles * split, 8) : up(up(tiles, 3) * split, 5));
             }
-            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 3.91f : 2.96f) + (outputs + 4.f * outputs * (float)split) * (1.f / 6.87e6f) : 0.f);
-            if (rest + std::max(work, stream) >= best) continue;
+            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 3.57f : 2.73f) + (outputs + 4.f * outputs * (float)split) * (1.f / 6.74e6f) : 0.f);
+            if (rest + std::max(work, stream) >= best) {
+                if (rest + stream >= best || work < 0.6f * stream) break;    // (more splits only add to the rest)
+                continue;
+            }
             const float t = rest + std::sqrt(std::sqrt(work * work * work * work + s4));
             if (t < best) {
                 best = t;
                 plan = {i, split, XB, YB};
             }
+            if (work < 0.6f * stream) break;
         }
     }
     return plan;
@@ -651,7 +657,7 @@ extern "C" rtn_status rtn_linear_w8a8(const void* dev_q, const float* dev_q_scal
     if (!rtn::aligned_to(dev_q_scales, 4)) return RTN_ERR_ALIGN;
     if (M == 0) return RTN_OK;
     const rtn::W8A8Plan plan = rtn::w8a8_plan(M, N, K, dev_workspace ? workspace_nbytes : 0);
-    if (!rtn::launchable(plan.workgroups(), 512) || (plan.split > 1 && !rtn::launchable((M * N / 4 + 255) / 256, 256)))
+    if (!rtn::launchable(plan.workgroups(), plan.threads()) || (plan.split > 1 && !rtn::launchable((M * N / 4 + 255) / 256, 256)))
         return RTN_ERR_SHAPE;
     const rtn::W8A8Params p = {static_cast<const int8_t*>(dev_q), dev_q_scales, static_cast<const uint8_t*>(dev_qweight), static_cast<const rtn::half_t*>(dev_scales),
                                dev_C, static_cast<int*>(dev_workspace), (int)M, (int)N, (int)(K / 64), (int)plan.XB, (int)plan.YB, plan.split};
