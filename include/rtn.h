@@ -403,13 +403,14 @@ rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int64_t q_stri
  *   scale = max|v| * (1 / 127),  code = rne(v * (1 / scale)), -127 .. 127, each operation one rounding in fp32; a row whose largest magnitude is below 2^-100 has
  *   scale 0 and codes 0.  (The norm's codes are those of h * weight, before the row's factor, which then multiplies the scale.)
  * 16-bit types: RTN_TYPE_F16, RTN_TYPE_BF16.  Rows of x are x_stride elements apart (a multiple of 8, at least their width), outputs are contiguous;
- * 0 .. 2^20 rows (0: nothing to do), dim a multiple of 8 up to 65536.  NaN or an infinity in a row gives unspecified results for that row, and for no
- * other.  Of dev_out (16 bits) and dev_q (codes, with dev_q_scales) exactly one is given.  No output may overlap an input, but for
+ * 0 .. 2^20 rows (0: nothing to do), dim a multiple of 8 up to 65536.  NaN, an infinity or a value v beyond fp32 in a row gives unspecified results for that
+ * row, and for no other.  Of dev_out (16 bits) and dev_q (codes, with dev_q_scales) exactly one is given.  No output may overlap an input, but for
  * dev_residual_out, which may be dev_residual or dev_x with the same stride. */
 enum { RTN_ACT_SILU = 0, RTN_ACT_GELU_TANH = 1 };
 
 /* The residual's addition and the root-mean-square norm: h = x + residual, rounded to the type and stored (without a residual h = x and nothing is
- * stored); v = h * rsqrt(mean(h^2) + eps) * weight.  Sums in fp32: magnitudes from 2^56 (bf16) on overflow them.  eps >= 0; a row of zeros gives zeros.
+ * stored); v = h * rsqrt(mean(h^2) + eps) * weight.  Sums in fp32: magnitudes from 2^56 (bf16) on overflow them; without eps rows
+ * that stay below 2^-60 (bf16) lose bits in them, down to zeros from 2^-75.  eps >= 0; a row of zeros gives zeros.
  *   dev_residual, dev_residual_out   in, out  [rows, dim], rows their strides apart; both or neither
  *   dev_weight   in   [dim], in the type */
 rtn_status rtn_norm_rows(const void* dev_x, int64_t rows, int64_t x_stride, int64_t dim, int dtype, const void* dev_residual, int64_t residual_stride,

@@ -59,8 +59,8 @@ __device__ __forceinline__ float quotient(float a, float d) {
     return fmaf(fmaf(-d, q, a), r, q);
 }
 
-// act(a) b.  Both activations are a / (1 + exp(-z)): z = a, or a (1 + 0.044715 a^2) sqrt(8 / pi), for which it is a / 2 (1 + tanh(z / 2)).  (At z = -88
-// the quotient is 2^-120; there it may as well stay.)
+// act(a) b.  Both activations are a / (1 + exp(-z)): z = a, or a (1 + 0.044715 a^2) sqrt(8 / pi), for which it is a / 2 (1 + tanh(z / 2)).  Below
+// z = -87.33 the divisor is beyond 2^126, its reciprocal counts as 0 and so does the result, whose magnitude is at most 87.4 / 2^126 |b|.
 template <bool GELU>
 __device__ __forceinline__ float gated(float a, float b) {
     const float z = GELU ? a * (1.0f + 0.044715f * a * a) * 1.59576912f : a;

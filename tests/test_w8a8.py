@@ -8,7 +8,8 @@ up to 2^-25.
   The norm's factor: a thread adds up to 64 squares, then 6 steps over lanes and 15 over wavefronts: the sum is off by at most 86 e, its square root by half of that;
   mean, rsqrt (one unit = 2 e), and two roundings behind it: 43 + 1 + 2 + 2, bounded by 50 e.
   The gate: gelu's z comes from two constants and five operations, each e, so that it is off by at most 7 e |z| (silu's z is exact), which exp carries over; exp's own error
-  2 e, 1 + exp, the quotient and the product with b 1 e each, and 3 e to spare: (8 + 7 |z|) e relative.  Below 2^-120 |b| results may vanish.
+  2 e, 1 + exp, the quotient and the product with b 1 e each, and 3 e to spare: (8 + 7 |z|) e relative.  Below z = -87.33 the divisor is beyond
+  2^126 and its reciprocal below the normal range, so that results of up to 87.4 / 2^126 < 2^-119 of |b| may vanish.
   The product: the sum is exact; it and its two products with scales are rounded in fp32: 3 e, and then u."""
 import numpy as np
 import pytest
@@ -256,20 +257,39 @@ def test_gated_rows(rtn, K, activation, dtype):
         rel = (8 + 7 * np.abs(z)) * E
         wo, o = _bordered(M, K, dtype)
         rtn.rtn_gated_rows(x, activation, out=o)
-        assert (np.abs(_f64(o) - v) <= (UNIT[dtype] + rel) * np.abs(v) + TINY[dtype] * (1 + np.abs(b))).all()
+        assert (np.abs(_f64(o) - v) <= (UNIT[dtype] + rel) * np.abs(v) + TINY[dtype] + 2.0 ** -119 * np.abs(b)).all()
         _sides_are_left(wo)
         wq, q = _bordered(M, K, torch.int8)
         ws, s = _bordered(M, 1, torch.float32)
         rtn.rtn_gated_rows(x, activation, quantize=True, out=(q, s.view(M)))
         _sides_are_left(wq, ws)
         most = np.abs(v).max(1)
-        off = (rel * np.abs(v)).max(1) + 2.0 ** -120 * np.abs(b).max(1)                # of any value, and so of the largest
+        off = (rel * np.abs(v)).max(1) + 2.0 ** -119 * np.abs(b).max(1)                # of any value, and so of the largest
         assert (np.abs(_f64(s)[:, 0] * 127 - most) <= off + 2 * E * most).all()
         some = most > 0
         assert (q.cpu().numpy()[~some] == 0).all() and (s.cpu().numpy()[~some] == 0).all()
         step = (most / 127)[some, None]
         far = np.abs(q.cpu().numpy()[some] - v[some] / step)
         assert (far <= 0.5 + 2 * off[some, None] / step + 127 * 4 * E).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("activation", ["silu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_gate_of_any_magnitude(rtn, dtype, activation):
+    most = torch.finfo(dtype).max
+    a = torch.tensor([-0.0, 0.0, 2.0 ** -24, -5.5, -10.0, -10.25, -16.0, -80.0, -87.0, -87.5, -88.0, -88.5, -89.0, -104.0, -1e4, -6e4, 6e4, 200.0] +
+                     [s * m for s in (1, -1) for m in (most, most / 3, most ** 0.5, most ** 0.25, most ** 0.125)] + [20.0] * 4, device=DEV).to(dtype)
+    for up in (1.0, -2.0 ** 10):
+        b = torch.full_like(a, up)
+        b[a.abs().float() > most / 2 ** 12] = 0.5            # (what leaves the type is not asked for)
+        x, y = _f64(a), _f64(b)
+        z = x if activation == "silu" else x * np.sqrt(8 / np.pi) * (1 + 0.044715 * x * x)
+        with np.errstate(over="ignore"):
+            v = x / (1 + np.exp(-z)) * y
+        got = _f64(rtn.rtn_gated_rows(torch.cat([a, b])[None], activation)[0])
+        rel = (8 + 7 * np.minimum(np.abs(z), 88)) * E        # beyond, the exponential is 0 or its reciprocal is
+        assert (np.abs(got - v) <= (UNIT[dtype] + rel) * np.abs(v) + TINY[dtype] + 2.0 ** -119 * np.abs(y)).all()
 
 
 @pytest.mark.gpu
