@@ -157,7 +157,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
 // LDS (piece_at); packed tiles lie as they are, a lane reads its own chunk.  Both come
 // straight into LDS, SA and SB steps ahead.  A step runs in phases of two row blocks and both halves of its columns; a phase reads the next one's operands, and
 // the one barrier of a step stands before its last phase, whose operands are in registers by then: the stage is free behind it, and the
-// requests for it go out over the phases that follow.  8192 rows of 28672 x 4096 700 to 750 us on different cards (2.6 to 2.75 PFLOP/s), 8192 x 8192 x 8192 373
+// requests for it go out over the phases that follow.  8192 rows of 28672 x 4096 700 to 770 us on different cards (2.5 to 2.75 PFLOP/s), 8192 x 8192 x 8192 373
 // to 399 (2.95), where the vendor library's int8 product takes 988 and 445; matrix cores 69 % busy at 1.65 GHz.  Turning weights into operands
 // costs 6 % of that.  A round of tiles begins and ends for 5 us (K = 4096: 10 %): workgroups that stay and request the next tile's first steps under the last
 // one's end have registers for two stages of weights only, and lose more on every step than they gain (749 -> 791; K = 512 170 -> 161). ----
