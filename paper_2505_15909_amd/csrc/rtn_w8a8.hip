@@ -368,18 +368,19 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
 
 // ---- Rows between: bound by the stream of weights where enough of them is on its way.  The eight wavefronts of a workgroup stand 8 / WK along N and WK along K.
 // A wavefront has NT tile rows of weights, straight into registers; the activations, 16 MB rows, come into LDS once for the wavefronts along N.
-// A step is 128 columns for each wavefront along K; both are requested S - 1 steps ahead, and one barrier a step says that its activations have landed
-// and the last one's are used up.  The wavefronts along K add up in LDS at the end, so that a small matrix fills the chip without a join: 217 rows of 4096 x 4096 10.6 us
+// A step is 128 columns for each wavefront along K; both are requested two steps ahead, and one barrier a step says that its activations have landed
+// and the last one's are used up.  The waits before it count loads, so what they leave on its way is always one whole request, which a barrier to the
+// scheduler closes; the last steps request nothing, since of what nobody multiplies the compiler keeps the loads into LDS alone.  The wavefronts along K add up in LDS at the end, so that a small matrix fills the chip without a join: 217 rows of 4096 x 4096 10.6 us
 // (two along K, 256 workgroups; one 16.1, tiles 20.7), 128 rows 8.3 (four).  64 rows of 28672 x 4096 22 us (5.5 TB/s), 128 rows 28.  ONCE: the weights are marked as read once -- one row tile, or more weights
 // than the L2s hold: 64 rows of 8192 x 28672 43.9 us, 46.8 unmarked; marked where two row tiles share them, 128 rows of 4096 x 4096 take 9.6 for 8.3,
 // 160 of 5120 x 5120 14.0 for 12.0. ----
-template <int TYPE, int MB, int NT, int WK, int S, bool ONCE>
-__global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) void w8a8_block_kernel(const W8A8Params p) {
+template <int TYPE, int MB, int NT, int WK, bool ONCE>
+__global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK <= 8 ? 4 : 2) void w8a8_block_kernel(const W8A8Params p) {
     constexpr int WN = 8 / WK, NA = MB * WK / 4, EACH = NA + 2 * NT;         // requests of a wavefront and step: of activations, in all
     constexpr int A_BYTES = MB * WK * 2048;
     static_assert(MB * NT * 8192 * (WK - 1) / WK <= 2 * A_BYTES, "sums of the wavefronts along K");
-    __shared__ __align__(16) uint8_t lds0[A_BYTES], lds1[A_BYTES], lds2[A_BYTES], lds3[S > 3 ? A_BYTES : 16];
-    auto stage = [&](int i) { return i == 0 ? lds0 : i == 1 ? lds1 : i == 2 ? lds2 : lds3; };
+    __shared__ __align__(16) uint8_t lds0[A_BYTES], lds1[A_BYTES], lds2[A_BYTES];
+    auto stage = [&](int i) { return i == 0 ? lds0 : i == 1 ? lds1 : lds2; };
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), nl = lane & 15, kq = lane >> 4;
     const int wn = wave % WN, wk = wave / WN;
     const int blocks = (p.XB * p.YB + kXcds - 1) / kXcds * kXcds, z = blockIdx.x / blocks;
@@ -405,7 +406,7 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
 #pragma unroll
     for (int j = 0; j < NT; ++j) b_lane[j] = j < b_tiles ? (uint32_t)j * (uint32_t)p.KT * 1024u + lane * 16 : kNoRow;
 
-    u32x4_t w[S][NT][2];
+    u32x4_t w[3][NT][2];
     auto request = [&](int u, int t) {                       // step t, into stage and registers u; units past the last one: the last, not multiplied
 #pragma unroll
         for (int i = 0; i < NA; ++i) load_to_lds(ra, stage(u) + (wave * NA + i) * 1024, a_lane[i], (s0 + around(begin + min(t * WK + a_unit[i], units - 1), units)) * 128);
@@ -422,11 +423,7 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
 #pragma unroll
         for (int j = 0; j < NT; ++j) acc[b][j] = (int4_t){0, 0, 0, 0};
     const uint32_t a_rd = (uint32_t)(wk * MB * 2048 + nl * 128), po[2] = {(uint32_t)((kq ^ (nl & 7)) * 16), (uint32_t)(((4 + kq) ^ (nl & 7)) * 16)};
-    auto step = [&](int u, int t) {
-        __builtin_amdgcn_sched_barrier(0);
-        wait_and_barrier<(S - 2) * EACH>();
-        __builtin_amdgcn_sched_barrier(0);
-        request((u + S - 1) % S, t + S - 1);
+    auto multiply = [&](int u, int t) {
         if (WK > 1 && t * WK + wk >= units) return;
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
@@ -441,18 +438,30 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK * S <= 40 ? 4 : 2) voi
             }
         }
     };
-#pragma unroll
-    for (int v = 0; v < S - 1; ++v) request(v, v);
-    // whole turns, then what is left: an exit within a turn would be, to the compiler's counts of loads, one more way into the next
+    auto landed_but_one = [&]() {                            // all requests have, but for the newest
+        __builtin_amdgcn_sched_barrier(0);
+        wait_and_barrier<EACH>();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    request(0, 0);
+    request(1, 1);
     int t = 0;
-    for (; t + S <= T; t += S) {
+    for (; t + 3 <= T; t += 3) {
 #pragma unroll
-        for (int u = 0; u < S; ++u) step(u, t + u);
+        for (int u = 0; u < 3; ++u) {
+            landed_but_one();
+            request((u + 2) % 3, t + u + 2);
+            multiply(u, t + u);
+        }
     }
-    const int left = T - t;
-#pragma unroll
-    for (int u = 0; u < S - 1; ++u)
-        if (u < left) step(u, t + u);
+    if (t < T) {                          // two requests are on their way, used or not
+        landed_but_one();
+        multiply(0, t);
+    }
+    if (T - t == 2) {
+        wait_and_barrier<0>();
+        multiply(1, t + 1);
+    }
     wait_and_barrier<0>();                // no load into LDS outlives the workgroup
 
     if constexpr (WK > 1) {
@@ -527,10 +536,10 @@ struct W8A8Shape {
 constexpr W8A8Shape kShapes[] = {
     {W8A8_STREAM, 1, 1, 16, 4, 3.81f, 0.257f, 0.34f}, {W8A8_STREAM, 1, 1, 8, 4, 3.53f, 0.127f, 0.21f},  {W8A8_STREAM, 1, 1, 8, 2, 3.52f, 0.177f, 0.143f},
     {W8A8_STREAM, 1, 2, 8, 2, 3.32f, 0.285f, 0.218f}, {W8A8_STREAM, 1, 4, 8, 2, 3.22f, 0.609f, 0.222f}, {W8A8_STREAM, 2, 2, 8, 2, 3.21f, 0.432f, 0.311f},
-    {W8A8_BLOCK, 2, 1, 4, 3, 3.52f, 0.494f, 0.f},     {W8A8_BLOCK, 2, 2, 4, 3, 3.45f, 0.815f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 3, 4.05f, 0.655f, 0.f},
-    {W8A8_BLOCK, 4, 1, 4, 3, 3.38f, 0.543f, 0.31f},   {W8A8_BLOCK, 4, 1, 2, 3, 4.01f, 0.395f, 0.168f},  {W8A8_BLOCK, 4, 1, 1, 3, 4.43f, 0.343f, 0.12f},
-    {W8A8_BLOCK, 4, 2, 2, 3, 4.75f, 0.797f, 0.082f},  {W8A8_BLOCK, 4, 2, 1, 3, 5.02f, 0.743f, 0.f},     {W8A8_BLOCK, 8, 1, 1, 3, 6.59f, 0.555f, 0.088f},
-    {W8A8_BLOCK, 8, 2, 2, 3, 7.39f, 1.017f, 0.227f},  {W8A8_BLOCK, 8, 2, 1, 3, 7.55f, 0.92f, 0.056f},   {W8A8_TILE, 4, 0, 0, 0, 5.53f, 0.715f, 0.169f},
+    {W8A8_BLOCK, 2, 1, 4, 0, 3.52f, 0.494f, 0.f},     {W8A8_BLOCK, 2, 2, 4, 0, 3.45f, 0.815f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 0, 4.05f, 0.655f, 0.f},
+    {W8A8_BLOCK, 4, 1, 4, 0, 3.38f, 0.543f, 0.31f},   {W8A8_BLOCK, 4, 1, 2, 0, 4.01f, 0.395f, 0.168f},  {W8A8_BLOCK, 4, 1, 1, 0, 4.43f, 0.343f, 0.12f},
+    {W8A8_BLOCK, 4, 2, 2, 0, 4.75f, 0.797f, 0.082f},  {W8A8_BLOCK, 4, 2, 1, 0, 5.02f, 0.743f, 0.f},     {W8A8_BLOCK, 8, 1, 1, 0, 6.59f, 0.555f, 0.088f},
+    {W8A8_BLOCK, 8, 2, 2, 0, 7.39f, 1.017f, 0.227f},  {W8A8_BLOCK, 8, 2, 1, 0, 7.55f, 0.92f, 0.056f},   {W8A8_TILE, 4, 0, 0, 0, 5.53f, 0.715f, 0.169f},
     {W8A8_TILE, 8, 0, 0, 0, 7.3f, 1.063f, 0.405f}};
 // Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
 // A tile kernel's one row tile, which has the weights to itself, the last.
@@ -616,8 +625,8 @@ static void launch_shape(const W8A8Params& p, dim3 grid, hipStream_t st) {
     constexpr W8A8Shape k = kShapes[I];
     if constexpr (k.kind == W8A8_STREAM) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, k.mb, k.nt, k.wk, k.depth>), grid, dim3(k.wk * 64), 0, st, p);
     else if constexpr (k.kind == W8A8_BLOCK) {
-        if (p.YB == 1 || !weights_near(p.N, (int64_t)p.KT * 64)) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, k.depth, true>), grid, dim3(512), 0, st, p);
-        else hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, k.depth, false>), grid, dim3(512), 0, st, p);
+        if (p.YB == 1 || !weights_near(p.N, (int64_t)p.KT * 64)) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, true>), grid, dim3(512), 0, st, p);
+        else hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, false>), grid, dim3(512), 0, st, p);
     }
     else hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, k.mb>), grid, dim3(kTileThreads), 0, st, p);
 }
