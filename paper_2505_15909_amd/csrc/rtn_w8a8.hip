@@ -4,12 +4,8 @@
 // tile is 16 rows x 64 columns and lane (row, quarter kq) owns the columns 8 kq .. and 32 + 8 kq .., codes + 128.  Two v_permlane16_swap
 // bring the eights of neighbouring quarters together, so that quarters 0 .. 3 hold the sixteens 0, 2, 1, 3, which are 16 bytes in a row of
 // row-major activations; four v_xor take the 128 off.
-#include <algorithm>
-#include <array>
-#include <cmath>
-#include <utility>
-
 #include "rtn_paged.h"
+#include "rtn_w8a8_plan.h"
 
 namespace rtn {
 
@@ -161,8 +157,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
 // to 399 (2.95), where the vendor library's int8 product takes 988 and 445; matrix cores 69 % busy at 1.65 GHz.  Turning weights into operands
 // costs 6 % of that.  A round of tiles begins and ends for 5 us (K = 4096: 10 %): workgroups that stay and request the next tile's first steps under the last
 // one's end have registers for two stages of weights only, and lose more on every step than they gain (749 -> 791; K = 512 170 -> 161). ----
-constexpr int kTileN = 256, kTileThreads = 512;
-constexpr int kZGroup = 4;
+constexpr int kTileThreads = 512, kZGroup = 4;
 
 // 16 bytes per lane from global memory into 1 KiB of LDS at a wave-uniform address
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, uint8_t* lds, uint32_t lane_off, int off) {
@@ -501,8 +496,6 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK <= 8 ? 4 : 2) void w8a
     }
 }
 
-constexpr int kMostSplits = 8;
-
 // Sums of the K splits' parts, four columns a thread.
 template <int TYPE>
 __global__ __launch_bounds__(256) void w8a8_join_kernel(const W8A8Params p) {
@@ -518,101 +511,6 @@ __global__ __launch_bounds__(256) void w8a8_join_kernel(const W8A8Params p) {
 #pragma unroll
     for (int z = 1; z < kMostSplits; ++z) s += part[z];
     *reinterpret_cast<u32x2_t*>(static_cast<half_t*>(p.C) + at) = four_results<TYPE>(s, row_scale, scale);
-}
-
-constexpr size_t kW8A8Workspace = (size_t)64 << 20;
-
-// The kernels' shapes and what their time is made of, in us.  Stream and block kernels: start + units x (workgroups on the fullest compute unit) x
-// (each + more x the share of a workgroup's rows that M has), a unit being the 64 (128) columns of a step of each wavefront along K: a compute unit
-// has some 32 KiB on their way at once, 50 to 65 GB/s where they come from beyond its L2, whatever the workgroups on it.  Tile kernels: rounds of one workgroup
-// a compute unit, whose step takes `each` where half the chip is busy and `each + more` where all of it is (power).  That against the weights' stream,
-// and a K split's join.  Fitted to 57 000 launches over 2000 problems (1 to 8192 rows, 128 to 57344 columns, K 768 to 28672): 7 to 13 % rms (19 for
-// 16 wavefronts along K), and the pick is 2 % behind the best of all launches on the mean (1 % from 129 rows, 3.5 % up to 40 rows and below 2000 columns), 32 % at most.
-enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
-struct W8A8Shape {
-    int kind, mb, nt, wk, depth;
-    float start, each, more;
-};
-constexpr W8A8Shape kShapes[] = {
-    {W8A8_STREAM, 1, 1, 16, 4, 3.81f, 0.257f, 0.34f}, {W8A8_STREAM, 1, 1, 8, 4, 3.53f, 0.127f, 0.21f},  {W8A8_STREAM, 1, 1, 8, 2, 3.52f, 0.177f, 0.143f},
-    {W8A8_STREAM, 1, 2, 8, 2, 3.32f, 0.285f, 0.218f}, {W8A8_STREAM, 1, 4, 8, 2, 3.22f, 0.609f, 0.222f}, {W8A8_STREAM, 2, 2, 8, 2, 3.21f, 0.432f, 0.311f},
-    {W8A8_BLOCK, 2, 1, 4, 0, 3.52f, 0.494f, 0.f},     {W8A8_BLOCK, 2, 2, 4, 0, 3.45f, 0.815f, 0.f},     {W8A8_BLOCK, 2, 2, 2, 0, 4.05f, 0.655f, 0.f},
-    {W8A8_BLOCK, 4, 1, 4, 0, 3.38f, 0.543f, 0.31f},   {W8A8_BLOCK, 4, 1, 2, 0, 4.01f, 0.395f, 0.168f},  {W8A8_BLOCK, 4, 1, 1, 0, 4.43f, 0.343f, 0.12f},
-    {W8A8_BLOCK, 4, 2, 2, 0, 4.75f, 0.797f, 0.082f},  {W8A8_BLOCK, 4, 2, 1, 0, 5.02f, 0.743f, 0.f},     {W8A8_BLOCK, 8, 1, 1, 0, 6.59f, 0.555f, 0.088f},
-    {W8A8_BLOCK, 8, 2, 2, 0, 7.39f, 1.017f, 0.227f},  {W8A8_BLOCK, 8, 2, 1, 0, 7.55f, 0.92f, 0.056f},   {W8A8_TILE, 4, 0, 0, 0, 5.53f, 0.715f, 0.169f},
-    {W8A8_TILE, 8, 0, 0, 0, 7.3f, 1.063f, 0.405f}};
-// Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
-// A tile kernel's one row tile, which has the weights to itself, the last.
-constexpr float kSharedStream = 1.200f, kSharedNear = 0.715f, kSharedFar = 0.979f, kTileAlone = 1.073f;
-constexpr int kShapeCount = sizeof(kShapes) / sizeof(kShapes[0]);
-
-struct W8A8Plan {
-    int shape, split;
-    int64_t XB, YB;
-    int threads() const { return kShapes[shape].kind == W8A8_STREAM ? kShapes[shape].wk * 64 : 512; }
-    int64_t workgroups() const { return (kShapes[shape].kind == W8A8_STREAM ? XB * YB : (XB * YB + kXcds - 1) / kXcds * kXcds) * split; }
-};
-
-constexpr int log2_const(int n) { return n > 1 ? 1 + log2_const(n / 2) : 0; }
-
-// What a shape covers, as powers of two: a workgroup's rows and columns, a unit's columns of K, wavefronts along K.
-struct W8A8Cover { int rows, columns, unit, along; };
-constexpr W8A8Cover cover_of(const W8A8Shape& k) {
-    return k.kind == W8A8_TILE ? W8A8Cover{log2_const(32 * k.mb), log2_const(kTileN), 8, 0}
-                               : W8A8Cover{log2_const(16 * k.mb), log2_const(k.kind == W8A8_BLOCK ? 128 * k.nt / k.wk : 16 * k.nt), k.kind == W8A8_BLOCK ? 7 : 6, log2_const(k.wk)};
-}
-template <int... I>
-constexpr std::array<W8A8Cover, sizeof...(I)> covers(std::integer_sequence<int, I...>) { return {cover_of(kShapes[I])...}; }
-constexpr auto kCovers = covers(std::make_integer_sequence<int, kShapeCount>());
-
-// Weights that the L2s hold together: row tiles that share them find them there.
-static bool weights_near(int64_t N, int64_t K) { return N * K <= (int64_t)32 << 20; }
-
-static W8A8Plan w8a8_plan(int64_t M, int64_t N, int64_t K, size_t workspace) {
-    W8A8Plan plan = {};
-    float best = 1e30f;
-    const float MN = (float)M * (float)N, outputs = 2.f * MN, stream = ((float)N + (float)M) * (float)K * (1.f / 7.14e6f);
-    const float s4 = stream * stream * stream * stream;
-    const int splits = (int)std::min<uint64_t>(kMostSplits, std::min(workspace, kW8A8Workspace) / 4 / (uint64_t)(M * N));
-    const int pieces = (int)((M + 15) / 16);
-    const bool near = weights_near(N, K);
-    auto up = [](int64_t n, int log2) { return (n + ((int64_t)1 << log2) - 1) >> log2; };
-    for (int i = 0; i < kShapeCount; ++i) {
-        const W8A8Shape& k = kShapes[i];
-        const W8A8Cover& c = kCovers[i];
-        if ((1 << c.rows) >= 32 * pieces && c.rows > 5) continue;            // mostly rows beyond M
-        if (k.kind != W8A8_TILE && pieces > (near ? 128 : 8) << (c.rows - 4)) continue;      // (that many times the weights)
-        const int64_t XB = up(N, c.columns), YB = up(M, c.rows), tiles = XB * YB, all_units = K >> c.unit;
-        const float shared = YB == 1 ? 1.f : k.kind == W8A8_STREAM ? kSharedStream : near ? kSharedNear : kSharedFar;
-        const float unit_us = (k.each + k.more * (float)M / (float)(YB << c.rows)) * shared;
-        const float once = k.start + (k.kind == W8A8_TILE ? 0.f : outputs * (1.f / 3.06e6f));
-        for (int split = 1; split <= std::max(1, splits); ++split) {
-            if (split > 1 && ((split << c.along) > all_units || tiles * split > 800)) break;
-            const float steps = (float)up((uint32_t)(all_units + split - 1) / (uint32_t)split, c.along);
-            float work;
-            if (k.kind == W8A8_TILE) {
-                const int64_t on_xcd = up(tiles, 3) * split;
-                const float part = (float)(on_xcd & 31) * (1.f / 32.f);
-                work = (float)(on_xcd >> 5) * (2.f * steps * (k.each + k.more) + 4.91f) - 4.91f;
-                if (part > 0.f) work += 2.f * steps * (k.each + k.more * std::max(0.f, 2.f * part - 1.f)) + 4.91f;
-                if (YB == 1) work *= kTileAlone;
-            } else {
-                work = steps * unit_us * (float)(k.kind == W8A8_STREAM ? up(tiles * split, 8) : up(up(tiles, 3) * split, 5));
-            }
-            const float rest = once + (split > 1 ? (k.kind == W8A8_TILE ? 3.57f : 2.73f) + (outputs + 4.f * outputs * (float)split) * (1.f / 6.74e6f) : 0.f);
-            if (rest + std::max(work, stream) >= best) {
-                if (rest + stream >= best || work < 0.6f * stream) break;    // (more splits only add to the rest)
-                continue;
-            }
-            const float t = rest + std::sqrt(std::sqrt(work * work * work * work + s4));
-            if (t < best) {
-                best = t;
-                plan = {i, split, XB, YB};
-            }
-            if (work < 0.6f * stream) break;
-        }
-    }
-    return plan;
 }
 
 static rtn_status check_w8a8(int64_t M, int64_t N, int64_t K) {

@@ -1,9 +1,17 @@
-"""The 8-bit layer's product, kernel by kernel: what the compiler made of the counted waits, by the code of the built library (no GPU)."""
+"""The 8-bit layer's product, kernel by kernel: what the compiler made of the counted waits, by the code of the built library, and which kernel a call takes, by a
+small host program around the plan (tests/host/w8a8_plan_driver.cpp); neither needs a GPU."""
 import bisect
+import math
+import os
 import re
 import subprocess
 
-from tests.test_host_plans import _code_objects
+import pytest
+
+from tests.test_host_plans import PKG, ROOT, _code_objects
+
+STREAM, BLOCK, TILE = range(3)
+WORKSPACE = 64 << 20
 
 
 def _events(tools, code_object, named):
@@ -93,3 +101,49 @@ def test_block_kernels_wait_for_whole_requests(tmp_path):
         if bad:
             wrong[name] = bad
     assert not wrong, wrong
+
+
+@pytest.fixture(scope="module")
+def plan(tmp_path_factory):
+    """plan([(M, N, K, bytes of workspace)]) -> [(shape, kind, split, workgroups along N, along M)]"""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    if not os.path.exists(hipcc):
+        pytest.skip("no hipcc")
+    exe = str(tmp_path_factory.mktemp("w8a8") / "plan")
+    subprocess.run([hipcc, "-O1", "-std=c++17", "--offload-arch=gfx950", "-x", "hip", "-o", exe, os.path.join(ROOT, "tests", "host", "w8a8_plan_driver.cpp")],
+                   check=True, capture_output=True, timeout=600)
+
+    def ask(problems):
+        out = subprocess.run([exe], input="".join("%d %d %d %d\n" % p for p in problems), check=True, capture_output=True, text=True, timeout=600).stdout.split("\n")
+        return [tuple(map(int, line.split())) for line in out if line]
+
+    return ask
+
+
+PROMPTS = [(M, N, K) for N, K in ((4096, 4096), (6144, 4096), (5120, 5120), (4096, 8192), (12288, 2048)) for M in (2576, 3000, 4112, 5000, 6144, 8192)]
+
+
+def test_prompts_take_the_tile_kernels(plan):
+    """Block kernels take 1.2 to 1.4 times as long there."""
+    for problem, (_, kind, *_) in zip(PROMPTS, plan([p + (WORKSPACE,) for p in PROMPTS])):
+        assert kind == TILE, problem
+
+
+@pytest.mark.parametrize("sweep,mean", [("w8a8_sweep_results.txt", 0.02), ("w8a8_sweep_heldout.txt", 0.03)])
+def test_picks_are_near_the_fastest_launch_measured(plan, sweep, mean):
+    """Over the sweeps that are kept (which leave out what takes more than 1.6 times as long as the fastest): how far the plan's launch is behind, on the mean of
+    logarithms; a split that was not measured counts as the slower of its neighbours."""
+    problems = []
+    for line in open(os.path.join(PKG, "tuning", sweep)):
+        if not line.startswith("#"):
+            head, *cells = line.split(" | ")
+            times = {tuple(map(int, c.split()[0].split("/"))): float(c.split()[1].rstrip("*")) for c in cells}
+            problems.append((tuple(map(int, head.split())), times))
+    assert len(problems) > 700
+    behind = []
+    for (problem, times), (shape, _, split, *_) in zip(problems, plan([p + (WORKSPACE,) for p, _ in problems])):
+        near = [(shape, split)] if split not in (5, 7) or (shape, split) in times else [(shape, split - 1), (shape, split + 1)]
+        took = [times[n] for n in near if n in times]
+        assert took, (problem, shape, split)
+        behind.append(math.log(max(took) / min(times.values())))
+    assert sum(behind) / len(behind) <= mean
