@@ -523,8 +523,10 @@ static void launch_shape(const W8A8Params& p, dim3 grid, hipStream_t st) {
     constexpr W8A8Shape k = kShapes[I];
     if constexpr (k.kind == W8A8_STREAM) hipLaunchKernelGGL((w8a8_stream_kernel<TYPE, k.mb, k.nt, k.wk, k.depth>), grid, dim3(k.wk * 64), 0, st, p);
     else if constexpr (k.kind == W8A8_BLOCK) {
-        if (p.YB == 1 || !weights_near(p.N, (int64_t)p.KT * 64)) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, true>), grid, dim3(512), 0, st, p);
-        else hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, false>), grid, dim3(512), 0, st, p);
+        // (128 rows x 256 columns are not chosen where row tiles share near weights)
+        constexpr bool near_too = k.mb * k.nt / k.wk < 16;
+        if (!near_too || p.YB == 1 || !weights_near(p.N, (int64_t)p.KT * 64)) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, true>), grid, dim3(512), 0, st, p);
+        else if constexpr (near_too) hipLaunchKernelGGL((w8a8_block_kernel<TYPE, k.mb, k.nt, k.wk, false>), grid, dim3(512), 0, st, p);
     }
     else hipLaunchKernelGGL((w8a8_tile_kernel<TYPE, k.mb>), grid, dim3(kTileThreads), 0, st, p);
 }

@@ -19,29 +19,28 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 // has some 32 KiB on their way at once, 50 to 65 GB/s where they come from beyond its L2, whatever the workgroups on it; and a block kernel's next round.  Tile kernels: rounds of one
 // workgroup a compute unit, whose step takes `each` where half the chip is busy and `each + more` where all of it is (power).  That against the weights' stream,
 // and a K split's join.  `depth`: a stream kernel's tiles on their way, the workgroups of a block kernel that a compute unit holds.
-// The constants are chosen for their picks, by tuning/w8a8_fit.py: the modelled times are 11 to 22 % off (rms).  2910 problems (1 to 8192 rows, 128 to 106496 columns, K 512 to 53248; tuning/w8a8_sweep.hip,
-// every shape with every split up to 8): the pick is 1.5 % behind the fastest launch on the mean, 5 to 12 % in one problem of twenty (most at 41 to 128 rows), 37 % at most (1620 rows of 240 x 3328); on
-// another card, problems that no constant was fitted to: 684 of the same ranges 2.4 % and 46 % (115 rows of 144 x 512), 100 of 512 to 8192 rows on matrices of layers within the L2s 1 % and 15 %.
+// The constants are chosen for their picks, by tuning/w8a8_fit.py: the modelled times are 12 to 22 % off (rms).  2910 problems (1 to 8192 rows, 128 to 106496 columns, K 512 to 53248; tuning/w8a8_sweep.hip,
+// every shape with every split up to 8): the pick is 1.4 % behind the fastest launch on the mean, 5 to 12 % in one problem of twenty (most at 41 to 128 rows), 26 % at most (384 rows of 6144 x 4096); on
+// another card, problems that no constant was fitted to: 684 of the same ranges 2.2 % and 46 % (115 rows of 144 x 512), 100 of 512 to 8192 rows on matrices of layers within the L2s 1 % and 15 %.
 enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
 struct W8A8Shape {
     int kind, mb, nt, wk, depth;
     float start, each, more;
 };
 constexpr W8A8Shape kShapes[] = {
-    {W8A8_STREAM, 1, 1, 16, 4, 3.385f, 0.337f, 0.357f}, {W8A8_STREAM, 1, 1, 8, 4, 2.114f, 0.184f, 0.201f},  {W8A8_STREAM, 1, 1, 8, 2, 1.692f, 0.382f, 0.004f},
-    {W8A8_STREAM, 1, 2, 8, 2, 1.777f, 0.374f, 0.184f},  {W8A8_STREAM, 1, 4, 8, 2, 2.361f, 0.709f, 0.144f},  {W8A8_STREAM, 2, 2, 8, 2, 2.765f, 0.362f, 0.25f},
-    {W8A8_BLOCK, 2, 1, 4, 3, 2.686f, 0.436f, 0.012f},   {W8A8_BLOCK, 2, 2, 4, 2, 3.109f, 0.752f, 0.001f},   {W8A8_BLOCK, 2, 2, 2, 2, 3.662f, 0.733f, 0.001f},
-    {W8A8_BLOCK, 4, 1, 4, 1, 2.701f, 0.58f, 0.153f},    {W8A8_BLOCK, 4, 1, 2, 3, 2.895f, 0.434f, 0.083f},   {W8A8_BLOCK, 4, 1, 1, 4, 2.952f, 0.428f, 0.006f},
-    {W8A8_BLOCK, 4, 2, 2, 2, 5.855f, 0.668f, 0.062f},   {W8A8_BLOCK, 4, 2, 1, 2, 6.461f, 0.572f, 0.002f},   {W8A8_BLOCK, 8, 1, 1, 3, 6.337f, 0.483f, 0.211f},
-    {W8A8_BLOCK, 8, 2, 2, 1, 8.447f, 0.576f, 0.485f},   {W8A8_BLOCK, 8, 2, 1, 1, 11.535f, 0.452f, 0.335f},  {W8A8_TILE, 4, 0, 0, 0, 5.612f, 0.702f, 0.035f},
-    {W8A8_TILE, 8, 0, 0, 0, 7.533f, 0.928f, 0.104f}};
+    {W8A8_STREAM, 1, 1, 16, 4, 3.424f, 0.326f, 0.358f}, {W8A8_STREAM, 1, 1, 8, 4, 2.141f, 0.18f, 0.198f},   {W8A8_STREAM, 1, 1, 8, 2, 1.727f, 0.375f, 0.004f},
+    {W8A8_STREAM, 1, 2, 8, 2, 1.813f, 0.367f, 0.181f},  {W8A8_STREAM, 1, 4, 8, 2, 2.39f, 0.694f, 0.138f},   {W8A8_STREAM, 2, 2, 8, 2, 2.788f, 0.355f, 0.24f},
+    {W8A8_BLOCK, 2, 1, 4, 3, 2.703f, 0.426f, 0.012f},   {W8A8_BLOCK, 2, 2, 4, 2, 3.154f, 0.727f, 0.001f},   {W8A8_BLOCK, 2, 2, 2, 2, 3.662f, 0.71f, 0.001f},
+    {W8A8_BLOCK, 4, 1, 4, 1, 2.563f, 0.423f, 0.433f},   {W8A8_BLOCK, 4, 1, 2, 3, 2.87f, 0.431f, 0.097f},    {W8A8_BLOCK, 4, 1, 1, 4, 2.937f, 0.434f, 0.008f},
+    {W8A8_BLOCK, 4, 2, 2, 2, 5.822f, 0.686f, 0.063f},   {W8A8_BLOCK, 4, 2, 1, 2, 6.576f, 0.585f, 0.001f},   {W8A8_BLOCK, 8, 2, 2, 1, 8.65f, 0.582f, 0.501f},
+    {W8A8_BLOCK, 8, 2, 1, 1, 11.428f, 0.476f, 0.326f},  {W8A8_TILE, 4, 0, 0, 0, 5.71f, 0.715f, 0.036f},     {W8A8_TILE, 8, 0, 0, 0, 7.557f, 0.942f, 0.109f}};
 // What a round of tiles and a further round of a block kernel's workgroups take beyond their steps, a join's launch and wait (us), and bytes a us.
-constexpr float kTileRound = 11.055f, kBlockRound = 3.424f;
-constexpr float kJoin = 2.640f, kJoinTile = 6.054f;
-constexpr float kStreamRate = 10.899e6f, kOutRate = 13.621e6f, kJoinRate = 5.628e6f;
+constexpr float kTileRound = 10.591f, kBlockRound = 3.301f;
+constexpr float kJoin = 2.585f, kJoinTile = 6.106f;
+constexpr float kStreamRate = 10.901e6f, kOutRate = 16.215e6f, kJoinRate = 5.442e6f;
 // Where row tiles share weights, times: in the stream kernels, whose wavefronts share nothing; in the block kernels, out of the L2s (32 MiB) and beyond.
 // A tile kernel's one row tile, which has the weights to itself, the last.
-constexpr float kSharedStream = 1.315f, kSharedNear = 0.984f, kSharedFar = 1.100f, kTileAlone = 1.263f;
+constexpr float kSharedStream = 1.322f, kSharedNear = 0.998f, kSharedFar = 1.102f, kTileAlone = 1.256f;
 // Block kernels for more than 128 rows only where tiles of 128 x 256 would leave half of the 256 compute units idle.  The faster of all block launches against the faster of all
 // tile launches: up to 64 such tiles block kernels win 92 problems of 100, 1.6 times as fast on the mean of all; 65 to 128 tiles 68, 1.08 times; more 8, and take 1.21 times as long
 // (6144 x 4096, 3000 rows: 92 us, the fastest block launch 92, the one that the model of block kernels alone preferred 119; 8192 rows 163 and 226).
