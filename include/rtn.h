@@ -400,8 +400,9 @@ rtn_status rtn_paged_attention(const void* dev_q, int64_t tokens, int64_t q_stri
  * three calls of rows below, in the order of a layer: norm -> qkv, quantise -> o, norm -> gate_up, gated activation -> down.
  *
  * Quantised rows: codes int8 [rows, dim], row-major and contiguous (8-byte aligned; 16 for the product); scales fp32 [rows].  Of the row's values v (those before any rounding to 16 bits):
- *   scale = max|v| * (1 / 127),  code = rne(v * (1 / scale)), -127 .. 127, each operation one rounding in fp32; a row whose largest magnitude is below 2^-100 has
- *   scale 0 and codes 0.  (The norm's codes are those of h * weight, before the row's factor, which then multiplies the scale.)
+ *   scale = max|v| * (1 / 127),  code = rne(v * (1 / scale)), -127 .. 127, each of these operations one rounding in fp32; a row whose largest magnitude is below 2^-100
+ *   has scale 0 and codes 0.  (The norm's codes are those of h * weight, before the row's factor, which then multiplies the scale; 2^-100 is compared with that.)
+ *   Plain rows' v is exact, the norm's factor and the gate come from a reciprocal root and an exponential that are good to about one unit of fp32.
  * 16-bit types: RTN_TYPE_F16, RTN_TYPE_BF16.  Rows of x are x_stride elements apart (a multiple of 8, at least their width), outputs are contiguous;
  * 0 .. 2^20 rows (0: nothing to do), dim a multiple of 8 up to 65536.  NaN, an infinity or a value v beyond fp32 in a row gives unspecified results for that
  * row, and for no other.  Of dev_out (16 bits) and dev_q (codes, with dev_q_scales) exactly one is given.  No output may overlap an input, but for

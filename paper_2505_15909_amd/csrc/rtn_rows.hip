@@ -4,8 +4,10 @@
 // Every one of them is v_k times a factor of the row: v = h w with the factor rsqrt(mean(h^2) + eps) for the norm, v = act(a) b and v = x
 // with 1.  The largest |v| and the sum of squares are found in one sweep and the codes are rne(v / (max|v| / 127)), which the factor does not
 // enter; so a row is read once, kept in registers, and meets once over the workgroup, not once for the norm and again for the scale.
-// h w is exact in fp32 (two significands of at most 11 bits); every other step is one rounding in fp32, in the order that the header of the entry points
-// gives, so that the codes of plain and normed rows are what the same steps give anywhere else.
+// Plain rows and their largest magnitude are exact, and h w is (two significands of at most 11 bits) unless it is below fp32's range; the step, its reciprocal and the value
+// times that are one rounding in fp32 each, in the order that the header of the entry points gives: the codes of plain and normed rows and the scales of plain ones are what
+// the same steps give anywhere else.  The norm's factor (sums in an order of their own, a reciprocal root to about one unit) and the gate (an exponential to about one unit)
+// are not, nor what they enter: the norm's scales and 16-bit results, and all that a gate gives.
 //
 // Bound by memory: the norm with a residual moves 7 bytes an element quantised, the gated activation 5, plain rows 3 (8192 x 8192 in 82 us,
 // 5.7 TB/s; 4096 x 28672 in 107 us, 5.5; 3001 x 16384 in 27.7, 5.3, where a copy of 1 GiB reaches 4.8 to 5.5).
@@ -45,14 +47,15 @@ __device__ __forceinline__ float wave_largest(float x) {
 
 #pragma clang fp contract(off)
 
-// exp(x) = 2^n 2^f with x log2(e) = n + f: the product's rounding and log2(e)'s second part go into f.  No special cases within +-88.
+// exp(x) = 2^n 2^f with x log2(e) = n + f, reduced with the constant in two parts as Cody and Waite do it: what the product rounds off and log2(e)'s second part go into
+// f, whose power the hardware has to about one unit.  No special cases within +-88.
 __device__ __forceinline__ float exp_within_88(float x) {
     const float t = x * 1.44269504f, n = __builtin_rintf(t);
     const float rest = fmaf(x, 1.92596299e-8f, fmaf(x, 1.44269504f, -t));
     return __builtin_amdgcn_ldexpf(__builtin_amdgcn_exp2f(t - n + rest), (int)n);
 }
 
-// a / d, rounded as a division is, for d >= 1: a reciprocal and a quotient with a step of correction each (5 instructions, 10 with the scaling
+// a / d, rounded as a division is, for 1 <= d < 2^126: Newton's step on a reciprocal and one correction of the quotient (5 instructions, 10 with the scaling
 // that a division of any two numbers needs).
 __device__ __forceinline__ float quotient(float a, float d) {
     const float r0 = __builtin_amdgcn_rcpf(d), r = fmaf(fmaf(-d, r0, 1.0f), r0, r0), q = a * r;
