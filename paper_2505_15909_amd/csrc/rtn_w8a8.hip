@@ -153,7 +153,7 @@ __global__ __launch_bounds__(WK * 64) void w8a8_stream_kernel(const W8A8Params p
 // LDS (piece_at); packed tiles lie as they are, a lane reads its own chunk.  Both come
 // straight into LDS, SA and SB steps ahead.  A step runs in phases of two row blocks and both halves of its columns; a phase reads the next one's operands, and
 // the one barrier of a step stands before its last phase, whose operands are in registers by then: the stage is free behind it, and the
-// requests for it go out over the phases that follow.  8192 rows of 28672 x 4096 700 to 770 us on different cards (2.5 to 2.75 PFLOP/s), 8192 x 8192 x 8192 373
+// requests for it go out over the phases that follow.  8192 rows of 28672 x 4096 700 to 785 us on different cards (2.45 to 2.75 PFLOP/s), 8192 x 8192 x 8192 373
 // to 399 (2.95), where the vendor library's int8 product takes 988 and 445; matrix cores 69 % busy at 1.65 GHz.  Turning weights into operands
 // costs 6 % of that.  A round of tiles begins and ends for 5 us (K = 4096: 10 %): workgroups that stay and request the next tile's first steps under the last
 // one's end have registers for two stages of weights only, and lose more on every step than they gain (749 -> 791; K = 512 170 -> 161). ----
@@ -366,7 +366,7 @@ __global__ __launch_bounds__(kTileThreads, 2) void w8a8_tile_kernel(const W8A8Pa
 // A step is 128 columns for each wavefront along K; both are requested two steps ahead, and one barrier a step says that its activations have landed
 // and the last one's are used up.  The waits before it count loads, so what they leave on its way is always one whole request, which a barrier to the
 // scheduler closes; the last steps request nothing, since of what nobody multiplies the compiler keeps the loads into LDS alone.  The wavefronts along K add up in LDS at the end, so that a small matrix fills the chip without a join: 217 rows of 4096 x 4096 10.6 us
-// (two along K, 256 workgroups; one 16.1, tiles 20.7), 128 rows 8.3 (four).  64 rows of 28672 x 4096 22 us (5.5 TB/s), 128 rows 28.  ONCE: the weights are marked as read once -- one row tile, or more weights
+// (two along K, 256 workgroups; one 16.1, tiles 20.7), 128 rows 8.3 (four; out of the last-level cache, from memory 10.4).  64 rows of 28672 x 4096 22.5 us (5.4 TB/s), 128 rows 30.  ONCE: the weights are marked as read once -- one row tile, or more weights
 // than the L2s hold: 64 rows of 8192 x 28672 43.9 us, 46.8 unmarked; marked where two row tiles share them, 128 rows of 4096 x 4096 take 9.6 for 8.3,
 // 160 of 5120 x 5120 14.0 for 12.0. ----
 template <int TYPE, int MB, int NT, int WK, bool ONCE>

@@ -21,7 +21,7 @@ constexpr size_t kW8A8Workspace = (size_t)64 << 20;
 // and a K split's join.  `depth`: a stream kernel's tiles on their way, the workgroups of a block kernel that a compute unit holds.
 // The constants are chosen for their picks, by tuning/w8a8_fit.py: the modelled times are 12 to 22 % off (rms).  2910 problems (1 to 8192 rows, 128 to 106496 columns, K 512 to 53248; tuning/w8a8_sweep.hip,
 // every shape with every split up to 8): the pick is 1.4 % behind the fastest launch on the mean, 5 to 12 % in one problem of twenty (most at 41 to 128 rows), 26 % at most (384 rows of 6144 x 4096); on
-// another card, problems that no constant was fitted to: 684 of the same ranges 2.2 % and 46 % (115 rows of 144 x 512), 100 of 512 to 8192 rows on matrices of layers within the L2s 1 % and 15 %.
+// another card, problems that no constant was fitted to: 684 of the same ranges 1.8 % and 25 % (115 rows of 144 x 512), 100 of 512 to 8192 rows on matrices of layers within the L2s 0.8 % and 16 %.
 enum { W8A8_STREAM, W8A8_BLOCK, W8A8_TILE };
 struct W8A8Shape {
     int kind, mb, nt, wk, depth;

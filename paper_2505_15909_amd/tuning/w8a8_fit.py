@@ -7,7 +7,7 @@
 
 A fit prints the constants as csrc/rtn_w8a8_plan.h has them, and for the launches that the fitted model picks the time over that of the fastest launch, as
 the logarithm of that ratio: mean and 95th percentile by rows, and the worst.  The model is the header's, its comment says what it is made of.
-w8a8_sweep_results.txt holds the sweeps of one card, shortened; the header's constants are fitted to those with their full lists.
+w8a8_sweep_results.txt holds the shortened sweeps that the header's constants are fitted to, w8a8_sweep_heldout.txt those of another card and other problems.
 """
 import math
 import os
@@ -19,7 +19,7 @@ import torch
 
 HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "csrc", "rtn_w8a8_plan.h")
 STREAM, BLOCK, TILE = range(3)
-SHAPES = [((STREAM, BLOCK, TILE)[["STREAM", "BLOCK", "TILE"].index(m[0])],) + tuple(map(int, m[1:5])) + tuple(map(float, m[5:8]))
+SHAPES = [(["STREAM", "BLOCK", "TILE"].index(m[0]),) + tuple(map(int, m[1:5])) + tuple(map(float, m[5:8]))
           for m in re.findall(r"\{W8A8_(\w+), (\d+), (\d+), (\d+), (\d+), ([\d.]+)f, ([\d.]+)f, ([\d.]+)f\}", open(HEADER).read())]
 COUNT = len(SHAPES)
 KIND, DEPTH = np.array([s[0] for s in SHAPES]), np.array([max(s[4], 1) for s in SHAPES])
