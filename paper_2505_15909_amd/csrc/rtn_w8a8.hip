@@ -440,6 +440,7 @@ __global__ __launch_bounds__(512, MB * NT <= 8 && MB * WK <= 8 ? 4 : 2) void w8a
     };
     request(0, 0);
     request(1, 1);
+    // whole turns, then what is left: an exit within a turn would be, to the compiler's counts of loads, one more way into the next
     int t = 0;
     for (; t + 3 <= T; t += 3) {
 #pragma unroll
